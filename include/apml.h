@@ -305,6 +305,136 @@ apml_status apml_profile_reset(void);
 apml_status apml_profile_read(int32_t n, double *total_ms, int64_t *count);
 const char *apml_phase_name(int32_t phase);
 
+/*
+ * Losses on features and on routed experts, for networks trained beside the
+ * loss above (descriptors of the points of two clouds matched to each other,
+ * tokens of a code book, segmentation classes, expert layers). Their calls
+ * allocate nothing, never synchronise and hold no state: temporaries lie in a
+ * workspace of the caller's, whose size a query gives (device memory, aligned
+ * to 256 bytes, free for other use once the call's kernels have run; two calls
+ * that may overlap need two), and what the backward pass needs of the forward
+ * one lies in a state array of the caller's. So every call can be captured into
+ * a graph. Gradients are overwritten. All sums are held in float32 or more.
+ */
+typedef enum { APML_F32 = 0, APML_BF16 = 1, APML_F16 = 2 } apml_dtype;
+typedef enum { APML_I64 = 0, APML_I32 = 1 } apml_index_type;
+typedef enum { APML_REDUCE_NONE = 0, APML_REDUCE_SUM = 1, APML_REDUCE_MEAN = 2 } apml_reduction;
+
+/*
+ * Softmax cross entropy of rows against classes by their scaled products,
+ * without storing the rows x classes logits. Per sample (the samples are
+ * independent problems; classes shared by all rows: samples = 1):
+ *
+ *   z_tv   = scale <x_t, w_v>
+ *   lse_t  = log sum_v exp z_tv
+ *   loss_t = lse_t - z_t,target_t + z_weight lse_t^2, 0 where target_t == ignore_index
+ *
+ * reduction SUM adds all rows' losses, MEAN divides by the rows that are not
+ * ignored (the loss is 0 where all are). An ignored row adds nothing and gets a
+ * zero gradient, whatever x holds there. A target outside [0, classes) other
+ * than ignore_index gives a NaN loss for its row, NaN gradients of that row and
+ * of w.
+ */
+typedef struct apml_linear_ce_desc {
+    uint32_t struct_size; /* sizeof(apml_linear_ce_desc) */
+    int32_t dtype;        /* apml_dtype of x, w, grad_x and grad_w */
+    int32_t target_type;  /* apml_index_type of target */
+    int32_t samples;      /* >= 1 */
+    int32_t rows;         /* >= 1, per sample; samples * rows <= 2^26 */
+    int32_t classes;      /* >= 1, <= 2^26 */
+    int32_t dim;          /* >= 1, <= 2^20 */
+    int32_t reduction;    /* apml_reduction */
+    float scale;          /* 1 / temperature */
+    float z_weight;       /* weight of lse^2 */
+    int64_t ignore_index;
+} apml_linear_ce_desc;
+
+/* samples 1, scale 1, z_weight 0, ignore_index -100, MEAN; the sizes 0. */
+void apml_linear_ce_desc_default(apml_linear_ce_desc *d);
+
+/* Bytes of workspace of the two calls for these x and w (their alignment
+ * decides whether they are copied into padded rows; NULL: the most any needs).
+ * Either pointer to a size may be NULL. */
+apml_status apml_linear_ce_workspace(const apml_linear_ce_desc *desc, const void *x, const void *w,
+                                     size_t *forward_bytes, size_t *backward_bytes);
+
+/*
+ *   x       device [samples][rows][dim] contiguous
+ *   w       device [samples][classes][dim] contiguous
+ *   target  device [samples][rows]
+ *   loss    device float32, [samples][rows] (NONE) or one value
+ *   state   device float32 [samples * rows + 1][4], aligned to 16 bytes, for
+ *           the backward pass, or NULL
+ */
+apml_status apml_linear_ce_forward(const apml_linear_ce_desc *desc, const void *x, const void *w, const void *target,
+                                   float *loss, float *state, void *workspace, size_t workspace_bytes,
+                                   apml_stream stream);
+
+/*
+ * Gradients of sum grad_loss * loss: grad_loss device float32 [samples][rows]
+ * (NONE) or one value; x, w, target and state as in the forward call. grad_x and
+ * grad_w (shapes of x and w, aligned to 16 bytes) are overwritten; one of them
+ * may be NULL. The logits' gradient exists in pieces of the classes (or of the
+ * samples), rounded to x's type for the two products that read it.
+ */
+apml_status apml_linear_ce_backward(const apml_linear_ce_desc *desc, const void *x, const void *w, const void *target,
+                                    const float *state, const float *grad_loss, void *grad_x, void *grad_w,
+                                    void *workspace, size_t workspace_bytes, apml_stream stream);
+
+/*
+ * Balance loss of a network with routed experts, and the tokens per expert.
+ * Per sample of `tokens` tokens, n of them valid, with p_t = softmax(logits_t):
+ *
+ *   counts_e = how often e stands in the valid tokens' chosen experts
+ *   f_e = counts_e / sum counts,   P_e = (1 / n) sum over valid t of p_te
+ *   loss = E sum_e f_e P_e + z_weight (1 / n) sum over valid t of lse_t^2
+ *
+ * 1 (without the second term) where tokens and probabilities are spread evenly.
+ * The gradient flows through the probabilities, not through the counts. A chosen
+ * expert outside [0, experts) is a dropped slot and counted nowhere. Tokens that
+ * are not valid add nothing and get a zero gradient, whatever logits holds
+ * there. A logit of -inf is an expert out of reach; a token with nothing else
+ * has no probabilities and adds nothing but its place in n. A sample without
+ * valid tokens has loss 0. SUM and MEAN are over the samples.
+ */
+typedef struct apml_balance_desc {
+    uint32_t struct_size; /* sizeof(apml_balance_desc) */
+    int32_t dtype;        /* apml_dtype of logits and grad_logits */
+    int32_t index_type;   /* apml_index_type of index */
+    int32_t samples;      /* >= 1, <= 2^20 */
+    int32_t tokens;       /* >= 1, per sample; samples * tokens <= 2^30 */
+    int32_t experts;      /* 1 to 1024 */
+    int32_t chosen;       /* >= 1, experts per token in index; tokens * chosen <= 2^30 */
+    int32_t reduction;    /* apml_reduction */
+    float z_weight;
+} apml_balance_desc;
+
+/* samples 1, chosen 1, z_weight 0, MEAN; the sizes 0. */
+void apml_balance_desc_default(apml_balance_desc *d);
+apml_status apml_balance_workspace(const apml_balance_desc *desc, size_t *bytes);
+
+/*
+ *   logits  device [samples][tokens][experts] contiguous
+ *   index   device [samples][tokens][chosen], or NULL: counts is given (the sum
+ *           over all ranks of what apml_expert_counts gave each, for instance)
+ *   valid   device [samples][tokens], a byte each, 0 for padding; or NULL
+ *   counts  device int64 [samples][experts], written, or read where index is NULL
+ *   loss    device float32 [samples] (NONE) or one value
+ *   state   device float32 [samples][experts + 1] for the backward pass, or NULL
+ */
+apml_status apml_balance_forward(const apml_balance_desc *desc, const void *logits, const void *index,
+                                 const uint8_t *valid, int64_t *counts, float *loss, float *state, void *workspace,
+                                 size_t workspace_bytes, apml_stream stream);
+
+/* Gradient of sum grad_loss * loss: grad_loss device float32 [samples] (NONE)
+ * or one value; grad_logits, of logits' shape and type, is overwritten. */
+apml_status apml_balance_backward(const apml_balance_desc *desc, const void *logits, const uint8_t *valid,
+                                  const float *state, const float *grad_loss, void *grad_logits, apml_stream stream);
+
+/* The counts alone; sizes and index as above. */
+apml_status apml_expert_counts(const void *index, int32_t index_type, const uint8_t *valid, int32_t samples,
+                               int32_t tokens, int32_t chosen, int32_t experts, int64_t *counts, apml_stream stream);
+
 const char *apml_status_string(apml_status status);
 /* Text of the last error on the calling thread ("" if none). */
 const char *apml_last_error(void);

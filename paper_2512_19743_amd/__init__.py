@@ -8,11 +8,16 @@ from ._lib import (  # noqa: F401
     DensePlan,
     Plan,
     apml_backward,
+    apml_balance_backward,
+    apml_balance_forward,
     apml_dense_backward,
     apml_dense_forward,
+    apml_expert_counts,
     apml_forward,
     apml_forward_backward_noalloc,
     apml_get_memory_stats,
+    apml_linear_ce_backward,
+    apml_linear_ce_forward,
     apml_params,
     apml_params_default,
     apml_profile_enable,
@@ -25,3 +30,4 @@ from ._lib import (  # noqa: F401
     load,
 )
 from .loss import APMLFunction, apml_loss, loss_params  # noqa: F401
+from .feature_losses import balance_loss, expert_counts, linear_ce_loss  # noqa: F401

@@ -53,6 +53,19 @@ class apml_plan_info(ctypes.Structure):
                 ("scanned_min", ctypes.c_int64), ("scanned_support", ctypes.c_int64)]
 
 
+class apml_linear_ce_desc(ctypes.Structure):
+    _fields_ = [("struct_size", ctypes.c_uint32), ("dtype", ctypes.c_int32), ("target_type", ctypes.c_int32),
+                ("samples", ctypes.c_int32), ("rows", ctypes.c_int32), ("classes", ctypes.c_int32),
+                ("dim", ctypes.c_int32), ("reduction", ctypes.c_int32), ("scale", ctypes.c_float),
+                ("z_weight", ctypes.c_float), ("ignore_index", ctypes.c_int64)]
+
+
+class apml_balance_desc(ctypes.Structure):
+    _fields_ = [("struct_size", ctypes.c_uint32), ("dtype", ctypes.c_int32), ("index_type", ctypes.c_int32),
+                ("samples", ctypes.c_int32), ("tokens", ctypes.c_int32), ("experts", ctypes.c_int32),
+                ("chosen", ctypes.c_int32), ("reduction", ctypes.c_int32), ("z_weight", ctypes.c_float)]
+
+
 class apml_memory_stats(ctypes.Structure):
     _fields_ = [("in_use", ctypes.c_int64), ("peak_in_use", ctypes.c_int64), ("reserved", ctypes.c_int64)]
 
@@ -98,6 +111,18 @@ def load() -> ctypes.CDLL:
         L.apml_profile_enable.argtypes = [i32]
         L.apml_profile_reset.argtypes = []
         L.apml_profile_read.argtypes = [i32, P(ctypes.c_double), P(i64)]
+        sz = ctypes.c_size_t
+        L.apml_linear_ce_desc_default.argtypes = [P(apml_linear_ce_desc)]
+        L.apml_linear_ce_desc_default.restype = None
+        L.apml_linear_ce_workspace.argtypes = [P(apml_linear_ce_desc), vp, vp, P(sz), P(sz)]
+        L.apml_linear_ce_forward.argtypes = [P(apml_linear_ce_desc), vp, vp, vp, vp, vp, vp, sz, vp]
+        L.apml_linear_ce_backward.argtypes = [P(apml_linear_ce_desc), vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+        L.apml_balance_desc_default.argtypes = [P(apml_balance_desc)]
+        L.apml_balance_desc_default.restype = None
+        L.apml_balance_workspace.argtypes = [P(apml_balance_desc), P(sz)]
+        L.apml_balance_forward.argtypes = [P(apml_balance_desc), vp, vp, vp, vp, vp, vp, vp, sz, vp]
+        L.apml_balance_backward.argtypes = [P(apml_balance_desc), vp, vp, vp, vp, vp, vp]
+        L.apml_expert_counts.argtypes = [vp, i32, vp, i32, i32, i32, i32, vp, vp]
         L.apml_phase_name.argtypes = [i32]
         L.apml_phase_name.restype = ctypes.c_char_p
         L.apml_status_string.argtypes = [ctypes.c_int]
@@ -110,7 +135,9 @@ def load() -> ctypes.CDLL:
                      "apml_dense_forward", "apml_dense_backward", "apml_dense_plan_destroy", "apml_plan_get_info",
                      "apml_plan_nnz", "apml_plan_export", "apml_plan_export_stats", "apml_set_allocator",
                      "apml_get_memory_stats", "apml_reset_peak_memory", "apml_release_cached_memory",
-                     "apml_profile_enable", "apml_profile_reset", "apml_profile_read"):
+                     "apml_profile_enable", "apml_profile_reset", "apml_profile_read", "apml_linear_ce_workspace",
+                     "apml_linear_ce_forward", "apml_linear_ce_backward", "apml_balance_workspace",
+                     "apml_balance_forward", "apml_balance_backward", "apml_expert_counts"):
             getattr(L, name).restype = ctypes.c_int
         _lib = L
         return L
@@ -360,6 +387,244 @@ def apml_dense_backward(plan: DensePlan, x: torch.Tensor, y: torch.Tensor, grad_
                                         _stream_handle(stream, x.device))
     _check("apml_dense_backward", st)
     return gx, gy
+
+
+_DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+_INDEX_TYPES = {torch.int64: 0, torch.int32: 1}
+_REDUCTIONS = {"none": 0, "sum": 1, "mean": 2}
+
+
+def _on_gpu(name: str, t: torch.Tensor, types, like: Optional[torch.Tensor] = None) -> torch.Tensor:
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise ValueError(f"{name} must be a tensor on a GPU (libapml has no CPU path)")
+    if t.dtype not in types:
+        raise ValueError(f"{name} must be {' or '.join(str(d).replace('torch.', '') for d in types)}, got {t.dtype}")
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    if like is not None and t.device != like.device:
+        raise ValueError(f"{name} must be on {like.device}, got {t.device}")
+    return t
+
+
+def _ptr(t: Optional[torch.Tensor]):
+    return ctypes.c_void_p(t.data_ptr()) if t is not None else None
+
+
+class _Queued:
+    """The device and stream of a call: what is allocated within belongs to that stream."""
+
+    def __init__(self, device: torch.device, stream: Optional[torch.cuda.Stream]):
+        if stream is not None and stream.device != device:
+            raise ValueError(f"stream must be on {device}, got {stream.device}")
+        self.guard = torch.cuda.stream(stream) if stream is not None else torch.cuda.device(device)
+        self.device, self.stream = device, stream
+
+    def __enter__(self):
+        self.guard.__enter__()
+        return _stream_handle(self.stream, self.device)
+
+    def __exit__(self, *exc):
+        return self.guard.__exit__(*exc)
+
+
+def _linear_ce_desc(x, w, target, scale, z_weight, ignore_index, reduction) -> apml_linear_ce_desc:
+    _on_gpu("x", x, _DTYPES)
+    _on_gpu("w", w, (x.dtype,), x)
+    _on_gpu("target", target, _INDEX_TYPES, x)
+    if reduction not in _REDUCTIONS:
+        raise ValueError(f"unknown reduction {reduction!r}")
+    if w.dim() not in (2, 3) or x.dim() < 2 or (w.dim() == 3 and (x.dim() != 3 or x.shape[0] != w.shape[0])):
+        raise ValueError("need x (..., dim) with w (classes, dim), or x (B, rows, dim) with w (B, classes, dim)")
+    if x.shape[-1] != w.shape[-1]:
+        raise ValueError("x and w must have the same dim")
+    if target.shape != x.shape[:-1]:
+        raise ValueError("target must have x's shape without its last dimension")
+    if w.shape[-2] < 1 or x.shape[-1] < 1:
+        raise ValueError("need at least one class and dim >= 1")
+    samples = w.shape[0] if w.dim() == 3 else 1
+    # no row: the caller launches nothing
+    rows = target.numel() // samples if samples else 0
+    if max(samples, rows, w.shape[-2], x.shape[-1]) >= 1 << 31:
+        raise ValueError("a size is beyond the library's 32-bit range")
+    return apml_linear_ce_desc(ctypes.sizeof(apml_linear_ce_desc), _DTYPES[x.dtype], _INDEX_TYPES[target.dtype], samples,
+                               rows, w.shape[-2], x.shape[-1], _REDUCTIONS[reduction], scale, z_weight, ignore_index)
+
+
+def apml_linear_ce_forward(x: torch.Tensor, w: torch.Tensor, target: torch.Tensor, *, scale: float = 1.0,
+                           z_weight: float = 0.0, ignore_index: int = -100, reduction: str = "mean",
+                           keep_state: bool = True, stream: Optional[torch.cuda.Stream] = None
+                           ) -> Tuple[torch.Tensor, Optional[torch.Tensor]]:
+    """Softmax cross entropy of x's rows against the classes w, float32: per row (reduction 'none',
+    target's shape) or one value; and, if keep_state, the state for apml_linear_ce_backward.
+
+    x (..., dim) with w (classes, dim), or x (B, rows, dim) with w (B, classes, dim): each sample with
+    classes of its own. float32, bfloat16 or float16; target int64 or int32, of x's leading shape.
+    """
+    d = _linear_ce_desc(x, w, target, scale, z_weight, ignore_index, reduction)
+    with _Queued(x.device, stream) as queue:
+        state = None
+        if d.rows == 0:
+            loss = torch.zeros(target.shape if reduction == "none" else (), dtype=torch.float32, device=x.device)
+            return loss, torch.empty(0, 4, dtype=torch.float32, device=x.device) if keep_state else None
+        loss = torch.empty(target.shape if reduction == "none" else (), dtype=torch.float32, device=x.device)
+        if keep_state:
+            state = torch.empty(d.samples * d.rows + 1, 4, dtype=torch.float32, device=x.device)
+        need = ctypes.c_size_t()
+        _check("apml_linear_ce_workspace",
+               load().apml_linear_ce_workspace(ctypes.byref(d), _ptr(x), _ptr(w), ctypes.byref(need), None))
+        ws = torch.empty(need.value, dtype=torch.uint8, device=x.device)
+        st = load().apml_linear_ce_forward(ctypes.byref(d), _ptr(x), _ptr(w), _ptr(target), _ptr(loss), _ptr(state),
+                                           _ptr(ws), need.value, queue)
+    _check("apml_linear_ce_forward", st)
+    return loss, state
+
+
+def apml_linear_ce_backward(state: torch.Tensor, x: torch.Tensor, w: torch.Tensor, target: torch.Tensor,
+                            grad_loss: torch.Tensor, *, scale: float = 1.0, z_weight: float = 0.0,
+                            ignore_index: int = -100, reduction: str = "mean", want_grad_x: bool = True,
+                            want_grad_w: bool = True, stream: Optional[torch.cuda.Stream] = None
+                            ) -> Tuple[Optional[torch.Tensor], Optional[torch.Tensor]]:
+    """Gradients of sum(grad_loss * loss) in x's type; the other arguments as in the forward call."""
+    d = _linear_ce_desc(x, w, target, scale, z_weight, ignore_index, reduction)
+    _on_gpu("grad_loss", grad_loss, (torch.float32,), x)
+    _on_gpu("state", state, (torch.float32,), x)
+    if grad_loss.numel() != (target.numel() if reduction == "none" else 1):
+        raise ValueError("grad_loss must have the loss's shape")
+    if not (want_grad_x or want_grad_w):
+        return None, None
+    if d.rows and state.numel() != 4 * (d.samples * d.rows + 1):
+        raise ValueError("state must come from the forward call on the same shapes")
+    with _Queued(x.device, stream) as queue:
+        make = torch.empty_like if d.rows else torch.zeros_like
+        gx = make(x) if want_grad_x else None
+        gw = make(w) if want_grad_w else None
+        if d.rows == 0:
+            return gx, gw
+        need = ctypes.c_size_t()
+        _check("apml_linear_ce_workspace",
+               load().apml_linear_ce_workspace(ctypes.byref(d), _ptr(x), _ptr(w), None, ctypes.byref(need)))
+        ws = torch.empty(need.value, dtype=torch.uint8, device=x.device)
+        st = load().apml_linear_ce_backward(ctypes.byref(d), _ptr(x), _ptr(w), _ptr(target), _ptr(state),
+                                            _ptr(grad_loss), _ptr(gx), _ptr(gw), _ptr(ws), need.value, queue)
+    _check("apml_linear_ce_backward", st)
+    return gx, gw
+
+
+def _routed(shape, what: str, t: torch.Tensor, lead) -> None:
+    if tuple(t.shape[:len(lead)]) != tuple(lead) or t.dim() != shape:
+        raise ValueError(f"{what} must have the tokens' shape {tuple(lead)} in front")
+
+
+def _balance_desc(logits, index, valid, z_weight, reduction) -> apml_balance_desc:
+    _on_gpu("logits", logits, _DTYPES)
+    if reduction not in _REDUCTIONS:
+        raise ValueError(f"unknown reduction {reduction!r}")
+    if logits.dim() not in (2, 3):
+        raise ValueError("logits must be (tokens, experts) or (B, tokens, experts)")
+    lead = logits.shape[:-1]
+    samples, tokens, experts = lead[0] if logits.dim() == 3 else 1, lead[-1], logits.shape[-1]
+    chosen, index_type = 1, torch.int64
+    if index is not None:
+        _on_gpu("experts", index, _INDEX_TYPES, logits)
+        _routed(logits.dim(), "experts", index, lead)
+        chosen, index_type = index.shape[-1], index.dtype
+        if chosen < 1:
+            raise ValueError("experts must name at least one expert a token")
+    if valid is not None:
+        _on_gpu("valid", valid, (torch.bool,), logits)
+        _routed(logits.dim() - 1, "valid", valid, lead)
+    if experts < 1 or samples < 1:
+        raise ValueError("need at least one sample and one expert")
+    if max(samples, tokens, experts, chosen) >= 1 << 31:
+        raise ValueError("a size is beyond the library's 32-bit range")
+    return apml_balance_desc(ctypes.sizeof(apml_balance_desc), _DTYPES[logits.dtype], _INDEX_TYPES[index_type], samples,
+                             tokens, experts, chosen, _REDUCTIONS[reduction], z_weight)
+
+
+def apml_balance_forward(logits: torch.Tensor, experts: Optional[torch.Tensor] = None, *,
+                         counts: Optional[torch.Tensor] = None, valid: Optional[torch.Tensor] = None,
+                         z_weight: float = 0.0, reduction: str = "mean", keep_state: bool = True,
+                         stream: Optional[torch.cuda.Stream] = None
+                         ) -> Tuple[torch.Tensor, torch.Tensor, Optional[torch.Tensor]]:
+    """Balance loss (float32, per sample or one value), the tokens per expert (int64) and, if keep_state,
+    the state for apml_balance_backward.
+
+    logits (B, tokens, experts) or (tokens, experts); experts (..., chosen), int64 or int32: the experts
+    of each token, or counts (B, experts) or (experts,): their tokens, int64; valid: bool, the tokens'
+    shape, False for padding.
+    """
+    if (experts is None) == (counts is None):
+        raise ValueError("give either experts or counts")
+    d = _balance_desc(logits, experts, valid, z_weight, reduction)
+    shape = logits.shape[:-2] + logits.shape[-1:]
+    if counts is not None:
+        _on_gpu("counts", counts, (torch.int64,), logits)
+        if counts.shape != shape:
+            raise ValueError(f"counts must have the shape {tuple(shape)}")
+    with _Queued(logits.device, stream) as queue:
+        lead = logits.shape[:-2] if reduction == "none" else ()
+        if d.tokens == 0:
+            if counts is None:
+                counts = torch.zeros(shape, dtype=torch.int64, device=logits.device)
+            loss = torch.zeros(lead, dtype=torch.float32, device=logits.device)
+            return loss, counts, torch.empty(0, dtype=torch.float32, device=logits.device) if keep_state else None
+        loss = torch.empty(lead, dtype=torch.float32, device=logits.device)
+        if counts is None:
+            counts = torch.empty(shape, dtype=torch.int64, device=logits.device)
+        state = torch.empty(d.samples, d.experts + 1, dtype=torch.float32, device=logits.device) if keep_state else None
+        need = ctypes.c_size_t()
+        _check("apml_balance_workspace", load().apml_balance_workspace(ctypes.byref(d), ctypes.byref(need)))
+        ws = torch.empty(need.value, dtype=torch.uint8, device=logits.device)
+        st = load().apml_balance_forward(ctypes.byref(d), _ptr(logits), _ptr(experts), _ptr(valid), _ptr(counts),
+                                         _ptr(loss), _ptr(state), _ptr(ws), need.value, queue)
+    _check("apml_balance_forward", st)
+    return loss, counts, state
+
+
+def apml_balance_backward(state: torch.Tensor, logits: torch.Tensor, grad_loss: torch.Tensor, *,
+                          valid: Optional[torch.Tensor] = None, z_weight: float = 0.0, reduction: str = "mean",
+                          stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """Gradient of sum(grad_loss * loss) in logits' type; the other arguments as in the forward call."""
+    d = _balance_desc(logits, None, valid, z_weight, reduction)
+    _on_gpu("grad_loss", grad_loss, (torch.float32,), logits)
+    _on_gpu("state", state, (torch.float32,), logits)
+    if grad_loss.numel() != (d.samples if reduction == "none" else 1):
+        raise ValueError("grad_loss must have the loss's shape")
+    if d.tokens and state.numel() != d.samples * (d.experts + 1):
+        raise ValueError("state must come from the forward call on the same shapes")
+    with _Queued(logits.device, stream) as queue:
+        grad = torch.empty_like(logits)
+        if d.tokens == 0:
+            return grad
+        st = load().apml_balance_backward(ctypes.byref(d), _ptr(logits), _ptr(valid), _ptr(state), _ptr(grad_loss),
+                                          _ptr(grad), queue)
+    _check("apml_balance_backward", st)
+    return grad
+
+
+def apml_expert_counts(experts: torch.Tensor, num_experts: int, *, valid: Optional[torch.Tensor] = None,
+                       stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """Tokens per expert, int64: (B, num_experts) for experts (B, tokens, chosen), (num_experts,) for
+    (tokens, chosen). Entries outside [0, num_experts) are dropped slots; tokens that are not valid are
+    padding."""
+    _on_gpu("experts", experts, _INDEX_TYPES)
+    if experts.dim() not in (2, 3):
+        raise ValueError("experts must be (tokens, chosen) or (B, tokens, chosen)")
+    if valid is not None:
+        _on_gpu("valid", valid, (torch.bool,), experts)
+        _routed(experts.dim() - 1, "valid", valid, experts.shape[:-1])
+    if max(*experts.shape, num_experts) >= 1 << 31 or num_experts < 1:
+        raise ValueError("num_experts must be at least 1, and every size below 2^31")
+    samples = experts.shape[0] if experts.dim() == 3 else 1
+    with _Queued(experts.device, stream) as queue:
+        shape = experts.shape[:-2] + (num_experts,)
+        if experts.numel() == 0:
+            return torch.zeros(shape, dtype=torch.int64, device=experts.device)
+        counts = torch.empty(shape, dtype=torch.int64, device=experts.device)
+        st = load().apml_expert_counts(_ptr(experts), _INDEX_TYPES[experts.dtype], _ptr(valid), samples,
+                                       experts.shape[-2], experts.shape[-1], num_experts, _ptr(counts), queue)
+    _check("apml_expert_counts", st)
+    return counts
 
 
 def apml_get_memory_stats() -> dict:

@@ -13,7 +13,8 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libapml.so")
-SOURCES = ["api.hip", "dense.hip", "spatial.hip", "cull.hip", "build.hip", "softmax.hip", "sinkhorn.hip", "dense_apml.hip"]
+SOURCES = ["api.hip", "dense.hip", "spatial.hip", "cull.hip", "build.hip", "softmax.hip", "sinkhorn.hip", "dense_apml.hip",
+           "linear_ce.hip", "balance.hip", "losses_api.hip"]
 ARCH = os.environ.get("APML_OFFLOAD_ARCH", "gfx950")
 
 FLAGS = [

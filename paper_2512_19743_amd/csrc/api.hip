@@ -35,6 +35,17 @@ apml_status fail(apml_status st, const std::string &msg)
     return st;
 }
 
+} // namespace
+
+apml_status apml::fail_with(apml_status st, const char *msg)
+{
+    return fail(st, msg);
+}
+
+void apml::clear_error() { g_last_error.clear(); }
+
+namespace {
+
 #define HIP_TRY(expr)                                                                          \
     do {                                                                                       \
         hipError_t e_ = (expr);                                                                \

@@ -1,0 +1,1067 @@
+// Softmax cross entropy of rows x_t against classes w_v, forward and backward,
+// without storing the logits z_tv = scale <x_t, w_v>:
+//
+//   lse_t  = log sum_v exp z_tv
+//   loss_t = lse_t - z_t,target + z_weight lse_t^2            (0 where ignored)
+//   dz_tv  = g_t ((1 + 2 z_weight lse_t) p_tv - [v = target]), p = exp(z - lse)
+//   dx     = scale dz w,   dw = scale dz^T x
+//
+// Four products of rows x classes x dim: z in the forward pass, z again in the
+// backward pass (by pieces, turned into dz in registers), dz w and dz^T x. All
+// run on one matrix-core kernel over 16-bit operands (k_product); what differs
+// is how each operand lies in memory and what becomes of the result.
+//
+// float32 operands are cut into three bfloat16 planes of 8 significant bits
+// each (exact: a = a0 + a1 + a2), and the product sums the six plane products
+// that reach 24 bits: a0 b0, a0 b1, a1 b0, a0 b2, a2 b0, a1 b1 (the rest is
+// below 2^-23 of a term). bfloat16 matrix instructions run at 16 times the rate
+// of float32 ones, so six of them cost 3/8 of one float32 product.
+#include <algorithm>
+
+#include "apml_internal.h"
+#include "device_common.h"
+#include "linear_ce.h"
+
+namespace apml {
+
+namespace {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+typedef short i16x4 __attribute__((ext_vector_type(4)));
+typedef short i16x8 __attribute__((ext_vector_type(8)));
+
+using lds_char = __attribute__((address_space(3))) char;
+
+// ---------------------------------------------------------------------------
+// 16-bit elements
+// ---------------------------------------------------------------------------
+
+struct Bf16 {
+    static constexpr float kUnit = 1.0f; // what 1 becomes in the stored gradient of the logits
+    static __device__ __forceinline__ uint16_t from(float v) { return __builtin_bit_cast(uint16_t, (__bf16)v); }
+    static __device__ __forceinline__ float to(uint16_t v) { return __builtin_bit_cast(float, (uint32_t)v << 16); }
+    static __device__ __forceinline__ f32x4 mma(i16x8 a, i16x8 b, f32x4 c)
+    {
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c,
+                                                       0, 0, 0);
+    }
+};
+
+struct F16 {
+    // Probabilities of many classes fall below half precision's range (2^-24 is
+    // its smallest step): with the values between -1 and 1 stored times 2^14,
+    // that step is 2^-38.
+    static constexpr float kUnit = 16384.0f;
+    static __device__ __forceinline__ uint16_t from(float v) { return __builtin_bit_cast(uint16_t, (_Float16)v); }
+    static __device__ __forceinline__ float to(uint16_t v) { return (float)__builtin_bit_cast(_Float16, v); }
+    static __device__ __forceinline__ f32x4 mma(i16x8 a, i16x8 b, f32x4 c)
+    {
+        return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0,
+                                                      0, 0);
+    }
+};
+
+// v cut into three bfloat16 values of 8 significant bits: v = a + b + c exactly
+// (truncated, so that no finite value becomes infinite).
+struct Planes {
+    uint16_t a, b, c;
+};
+__device__ __forceinline__ Planes planes_of(float v)
+{
+    const uint32_t ua = __builtin_bit_cast(uint32_t, v) & 0xffff0000u;
+    const float r = v - __builtin_bit_cast(float, ua);
+    const uint32_t ub = __builtin_bit_cast(uint32_t, r) & 0xffff0000u;
+    const float q = r - __builtin_bit_cast(float, ub);
+    return {(uint16_t)(ua >> 16), (uint16_t)(ub >> 16), (uint16_t)(__builtin_bit_cast(uint32_t, q) >> 16)};
+}
+
+// The plane products of a float32 product.
+constexpr int kPlaneProducts = 6;
+
+// ---------------------------------------------------------------------------
+// the product C[q][p] = sum_k P[p][k] Q[q][k]
+// ---------------------------------------------------------------------------
+
+// One operand: `rows` rows (the p or q axis) by `k` summed elements, either
+// with k contiguous (row r, element k at r * ld + k) or with the rows
+// contiguous (at k * ld + r). Rows beyond `rows` are read as the last one; the
+// results they give are not stored. ld is a multiple of 8 and the base 16-byte
+// aligned.
+struct Operand {
+    const uint16_t *base;
+    int64_t sample; // elements from one sample to the next
+    int64_t plane;  // and from one plane to the next
+    int64_t ld;
+    int rows;
+    int k;          // elements of the summed axis that may be read
+};
+
+struct Product {
+    Operand p, q;
+    int steps;       // steps of kCeStep along the summed axis
+    int tiles_p, tiles_q, samples, splits;
+    int group;       // q tiles that a run of workgroups stays within
+};
+
+__device__ __forceinline__ int k_swizzle(int k) { return ((k & 3) | ((k >> 1) & 4)) << 1; }
+
+// Byte offset, from the operand's base of a step, of what lane `lane` of load
+// `j` (1 KB of the tile) fetches. With k contiguous the tile holds ROWS rows of
+// 8 chunks of 16 bytes, chunk c of row r in slot c ^ (r & 7): the 16 rows that a
+// fragment read touches then lie in different banks. With the rows contiguous
+// it holds kCeStep rows of ROWS / 8 chunks, moved by k_swizzle for the same
+// reason (a transposing read touches the same columns of 16 rows).
+// The base is that of row first_row (a tile of the padded rows may begin behind
+// the last one).
+template <bool KS> __device__ __forceinline__ int first_row(const Operand &o, int r0)
+{
+    return min(r0, KS ? (o.rows - 1) & ~7 : o.rows - 1);
+}
+template <int ROWS, bool KS>
+__device__ __forceinline__ uint32_t tile_offset(const Operand &o, int r0, int j, int lane, int k_left)
+{
+    if constexpr (!KS) {
+        const int r = j * 8 + (lane >> 3);
+        const int c = (lane & 7) ^ (r & 7);
+        const int row = min(r0 + r, o.rows - 1);
+        return (uint32_t)((row - first_row<KS>(o, r0)) * o.ld + min(c, (k_left - 1) >> 3) * 8) * 2u;
+    } else {
+        constexpr int CH = ROWS / 8;
+        const int k = j * (64 / CH) + lane / CH;
+        const int c = (lane % CH) ^ k_swizzle(k);
+        const int col = min(r0 + c * 8, (o.rows - 1) & ~7);
+        return (uint32_t)(min(k, k_left - 1) * o.ld + (col - first_row<KS>(o, r0))) * 2u;
+    }
+}
+
+// Loads 16 bytes a lane straight into shared memory at lds + 16 lane. The
+// caller waits for it (s_waitcnt vmcnt) before the barrier that hands the tile
+// over; the compiler does not see it.
+__device__ __forceinline__ void load_to_lds(i32x4 rsrc, uint32_t offset, uint32_t lds)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds), "v"(offset),
+                 "s"(rsrc)
+                 : "memory");
+}
+
+__device__ __forceinline__ i32x4 buffer_at(uint64_t base)
+{
+    i32x4 r;
+    r.x = (int)(uint32_t)base;
+    r.y = (int)(uint32_t)(base >> 32) & 0xffff;
+    r.z = -1; // the offsets stay in the operand by tile_offset
+    r.w = 0x00020000;
+    return r;
+}
+
+template <int N> __device__ __forceinline__ void wait_loads()
+{
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+}
+__device__ __forceinline__ void wait_lds_and_meet()
+{
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+}
+
+// The 16 x 32 fragment of a tile at rows r .. r + 15 and elements 32 h ..:
+// lane l holds row l & 15, elements 8 (l >> 4) .. + 7.
+template <int ROWS, bool KS> __device__ __forceinline__ i16x8 fragment(const lds_char *tile, int r, int h, int lane)
+{
+    if constexpr (!KS) {
+        const int row = r + (lane & 15);
+        const int slot = (h * 4 + (lane >> 4)) ^ (row & 7);
+        return *(const __attribute__((address_space(3))) i16x8 *)(tile + row * 128 + slot * 16);
+    } else {
+        // a transposing read gives lane i of 16 the column i of 4 rows of 16
+        const int k = h * 32 + (lane >> 4) * 8 + ((lane & 15) >> 2);
+        const int col = r + (lane & 3) * 4;
+        const lds_char *at = tile + k * (ROWS * 2) + (((col >> 3) ^ k_swizzle(k)) << 4) + ((col & 7) << 1);
+        using v4 = __attribute__((address_space(3))) i16x4;
+        const i16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((v4 *)at);
+        const i16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((v4 *)(at + 4 * ROWS * 2));
+        return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+    }
+}
+
+// The tile shapes. A workgroup takes TP x TQ results, its waves WP x WQ of them.
+template <int TP_, int TQ_, int WP_, int WQ_, int BUFS_> struct Shape {
+    static constexpr int TP = TP_, TQ = TQ_, WP = WP_, WQ = WQ_, BUFS = BUFS_;
+    static constexpr int waves = WP * WQ, threads = 64 * waves;
+    static constexpr int SP = TP / WP / 16, SQ = TQ / WQ / 16; // 16 x 16 results of a wave
+    static constexpr int stage = (TP + TQ) * 128;
+    static constexpr int lds = stage * BUFS;
+    static constexpr int LP = TP / 8 / waves;                                    // loads of a wave for P
+    static constexpr int LQ = (TQ / 8 + waves - 1) / waves;                      // and for Q
+};
+
+struct Place {
+    int p0, q0, sample, split; // where a workgroup's tile starts
+    int wp, wq, lane;          // wave within the workgroup
+};
+
+// ELEM: the elements; PLANES: float32 operands in three planes; PK, QK: the
+// operand's rows are contiguous; Finish: what becomes of the results.
+template <class ELEM, bool PLANES, bool PK, bool QK, class S, class Finish>
+__global__ __launch_bounds__(S::threads) void k_product(Product a, Finish finish)
+{
+    extern __shared__ __attribute__((aligned(1024))) char smem[];
+    const int lane = lane_id();
+    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    Place at;
+    at.lane = lane;
+    at.wp = wave % S::WP;
+    at.wq = wave / S::WP;
+    {
+        // The workgroups of an XCD take a run of tiles; within it, `group` q
+        // tiles for one p tile after the other, so that the tiles in flight
+        // share rows of both operands in that XCD's L2.
+        int id = xcd_contiguous((int)blockIdx.x, (int)gridDim.x);
+        const int per = a.tiles_p * a.tiles_q;
+        at.split = id % a.splits;
+        id /= a.splits;
+        at.sample = id / per;
+        id -= at.sample * per;
+        const int g0 = id / (a.group * a.tiles_p) * a.group;
+        const int gn = min(a.group, a.tiles_q - g0);
+        id -= g0 * a.tiles_p;
+        at.p0 = id / gn * S::TP;
+        at.q0 = (g0 + id % gn) * S::TQ;
+    }
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_char *)smem;
+    // steps of this part of the sum
+    const int first = (int)((int64_t)a.steps * at.split / a.splits);
+    const int last = (int)((int64_t)a.steps * (at.split + 1) / a.splits);
+    const int n = last - first, total = PLANES ? n * kPlaneProducts : n;
+
+    uint32_t op[S::LP], oq[S::LQ];
+    const auto offsets = [&](int step) {
+        const int kp = min(kCeStep, a.p.k - step * kCeStep), kq = min(kCeStep, a.q.k - step * kCeStep);
+#pragma unroll
+        for (int j = 0; j < S::LP; ++j)
+            op[j] = tile_offset<S::TP, PK>(a.p, at.p0, wave * S::LP + j, lane, kp);
+#pragma unroll
+        for (int j = 0; j < S::LQ; ++j)
+            oq[j] = tile_offset<S::TQ, QK>(a.q, at.q0, (wave * S::LQ + j) % (S::TQ / 8), lane, kq);
+    };
+    const int64_t step_p = PK ? kCeStep * a.p.ld : kCeStep, step_q = QK ? kCeStep * a.q.ld : kCeStep;
+    const uint64_t base_p = (uint64_t)(a.p.base + at.sample * a.p.sample + first_row<PK>(a.p, at.p0) * (PK ? 1 : a.p.ld));
+    const uint64_t base_q = (uint64_t)(a.q.base + at.sample * a.q.sample + first_row<QK>(a.q, at.q0) * (QK ? 1 : a.q.ld));
+    // A step that ends beyond an operand's summed axis clamps its offsets.
+    const int ragged = (a.p.k < a.steps * kCeStep || a.q.k < a.steps * kCeStep) ? a.steps - 1 : -1;
+    offsets(0);
+    const auto load = [&](int i) {
+        int step = first + i, pp = 0, pq = 0;
+        if constexpr (PLANES) {
+            const int prod = i / n;
+            step = first + i - prod * n;
+            pp = (0x120100 >> (4 * prod)) & 15; // planes 0 0 1 0 2 1
+            pq = (0x102010 >> (4 * prod)) & 15; // planes 0 1 0 2 0 1
+        }
+        if (ragged >= 0 && (step == ragged || step == first))
+            offsets(step);
+        const i32x4 rp = buffer_at(base_p + 2 * (uint64_t)(step * step_p + pp * a.p.plane));
+        const i32x4 rq = buffer_at(base_q + 2 * (uint64_t)(step * step_q + pq * a.q.plane));
+        const uint32_t to = lds0 + (i % S::BUFS) * S::stage;
+#pragma unroll
+        for (int j = 0; j < S::LP; ++j)
+            load_to_lds(rp, op[j], to + (wave * S::LP + j) * 1024);
+#pragma unroll
+        for (int j = 0; j < S::LQ; ++j)
+            load_to_lds(rq, oq[j], to + S::TP * 128 + ((wave * S::LQ + j) % (S::TQ / 8)) * 1024);
+    };
+
+    f32x4 acc[S::SP][S::SQ];
+#pragma unroll
+    for (int i = 0; i < S::SP; ++i)
+#pragma unroll
+        for (int j = 0; j < S::SQ; ++j)
+            acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+
+    for (int i = 0; i < S::BUFS - 1 && i < total; ++i)
+        load(i);
+    for (int i = 0; i < total; ++i) {
+        // this step's tile has arrived once at most the later steps' loads are out
+        if (i + S::BUFS - 2 < total)
+            wait_loads<(S::BUFS - 2) * (S::LP + S::LQ)>();
+        else
+            wait_loads<0>();
+        wait_lds_and_meet(); // also: every wave has read the tile that the next load overwrites
+        if (i + S::BUFS - 1 < total)
+            load(i + S::BUFS - 1);
+        const lds_char *tp = (const lds_char *)smem + (i % S::BUFS) * S::stage, *tq = tp + S::TP * 128;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            i16x8 fp[S::SP], fq[S::SQ];
+#pragma unroll
+            for (int j = 0; j < S::SQ; ++j)
+                fq[j] = fragment<S::TQ, QK>(tq, at.wq * (S::SQ * 16) + j * 16, h, lane);
+#pragma unroll
+            for (int k = 0; k < S::SP; ++k)
+                fp[k] = fragment<S::TP, PK>(tp, at.wp * (S::SP * 16) + k * 16, h, lane);
+#pragma unroll
+            for (int k = 0; k < S::SP; ++k)
+#pragma unroll
+                for (int j = 0; j < S::SQ; ++j)
+                    acc[k][j] = ELEM::mma(fp[k], fq[j], acc[k][j]);
+        }
+    }
+    // lane l holds, of 16 x 16 results, q = l & 15 and p = 4 (l >> 4) .. + 3
+    finish.template operator()<ELEM, S>(a, at, acc);
+}
+
+// --- what becomes of the results -------------------------------------------
+
+// Forward: per row (q) the maximum and the sum of exp(z - max) over a wave's
+// classes (p), without the target's, whose logit is kept apart.
+struct FinishStats {
+    const int32_t *target; // [samples * rows], below 0 where there is none
+    float2 *part;          // [parts][samples * rows]
+    float *picked;         // [samples * rows]
+    float scale;
+    template <class ELEM, class S>
+    __device__ __forceinline__ void operator()(const Product &a, const Place &at, f32x4 (&acc)[S::SP][S::SQ]) const
+    {
+        const int g = at.lane >> 4;
+        const int v0 = at.p0 + at.wp * (S::SP * 16) + 4 * g;
+        const int64_t total = (int64_t)a.samples * a.q.rows;
+#pragma unroll
+        for (int j = 0; j < S::SQ; ++j) {
+            const int t = at.q0 + at.wq * (S::SQ * 16) + j * 16 + (at.lane & 15);
+            const int64_t row = (int64_t)at.sample * a.q.rows + t;
+            const bool in = t < a.q.rows;
+            const int target = in ? target_at(row) : -1;
+            float m = -kInf;
+#pragma unroll
+            for (int k = 0; k < S::SP; ++k)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int v = v0 + k * 16 + i;
+                    float z = acc[k][j][i] * scale;
+                    if (v == target)
+                        picked[row] = z;
+                    if (v == target || v >= a.p.rows)
+                        z = -kInf;
+                    acc[k][j][i] = z;
+                    m = fmaxf(m, z);
+                }
+            m = fmaxf(m, __shfl_xor(m, 16));
+            m = fmaxf(m, __shfl_xor(m, 32));
+            const float base = m == -kInf ? 0.0f : m;
+            float sum = 0.0f;
+#pragma unroll
+            for (int k = 0; k < S::SP; ++k)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    sum += __expf(acc[k][j][i] - base);
+            sum += __shfl_xor(sum, 16);
+            sum += __shfl_xor(sum, 32);
+            if (in && g == 0)
+                part[(int64_t)(at.p0 / S::TP * S::WP + at.wp) * total + row] = make_float2(m, sum);
+        }
+    }
+    __device__ __forceinline__ int target_at(int64_t row) const { return target[row]; }
+};
+
+// What the backward pass needs of a row: the logits' gradient is
+// fac exp(z - top), or at_target for the target's class, in units of the row's
+// power of two (unit); fac 0: an ignored row.
+struct CeCoef {
+    float top, fac, at_target, unit;
+};
+
+// Backward: the logits' gradient of a piece, rounded to the operands' type (the
+// products that follow take 16-bit operands; each value is off by half a step of
+// its own size at most, as the operands x and w themselves are), or in three
+// planes for float32.
+template <bool PLANES> struct FinishGrad {
+    const int32_t *target;
+    const CeCoef *coef;
+    uint16_t *g;         // [samples of the piece][rows_pad][ld]
+    int64_t plane;
+    float scale;
+    int rows_pad, ld, class0;
+    template <class ELEM, class S>
+    __device__ __forceinline__ void operator()(const Product &a, const Place &at, f32x4 (&acc)[S::SP][S::SQ]) const
+    {
+        const int c0 = at.p0 + at.wp * (S::SP * 16) + 4 * (at.lane >> 4);
+#pragma unroll
+        for (int j = 0; j < S::SQ; ++j) {
+            const int t = at.q0 + at.wq * (S::SQ * 16) + j * 16 + (at.lane & 15);
+            if (t >= rows_pad)
+                continue;
+            const int64_t row = (int64_t)at.sample * a.q.rows + t;
+            CeCoef c{0.0f, 0.0f, 0.0f, 0.0f};
+            int target = -1;
+            if (t < a.q.rows) {
+                c = coef[row];
+                target = this->target[row] - class0;
+            }
+#pragma unroll
+            for (int k = 0; k < S::SP; ++k) {
+                const int v = c0 + k * 16;
+                if (v >= ld)
+                    continue;
+                float d[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float e = __expf(acc[k][j][i] * scale - c.top);
+                    d[i] = v + i == target ? c.at_target : c.fac * e;
+                    if (c.fac == 0.0f || v + i >= a.p.rows)
+                        d[i] = 0.0f;
+                }
+                uint16_t *to = g + ((int64_t)at.sample * rows_pad + t) * ld + v;
+                if constexpr (PLANES) {
+                    const Planes x = planes_of(d[0]), y = planes_of(d[1]), z = planes_of(d[2]), u = planes_of(d[3]);
+                    *(ushort4 *)to = make_ushort4(x.a, y.a, z.a, u.a);
+                    *(ushort4 *)(to + plane) = make_ushort4(x.b, y.b, z.b, u.b);
+                    *(ushort4 *)(to + 2 * plane) = make_ushort4(x.c, y.c, z.c, u.c);
+                } else {
+                    *(ushort4 *)to = make_ushort4(ELEM::from(d[0]), ELEM::from(d[1]), ELEM::from(d[2]), ELEM::from(d[3]));
+                }
+            }
+        }
+    }
+};
+
+// OUT: the type of a gradient that goes out.
+template <class OUT> __device__ __forceinline__ void put(void *out, int64_t at, float v)
+{
+    ((uint16_t *)out)[at] = OUT::from(v);
+}
+template <> __device__ __forceinline__ void put<float>(void *out, int64_t at, float v) { ((float *)out)[at] = v; }
+
+template <class OUT> __device__ __forceinline__ void put4(void *out, int64_t at, f32x4 v)
+{
+    *(ushort4 *)((uint16_t *)out + at) = make_ushort4(OUT::from(v[0]), OUT::from(v[1]), OUT::from(v[2]), OUT::from(v[3]));
+}
+template <> __device__ __forceinline__ void put4<float>(void *out, int64_t at, f32x4 v) { *(f32x4 *)((float *)out + at) = v; }
+
+// A gradient [samples][q rows][p rows]: rounded once and stored, times a factor
+// per row (coef) or for all (top).
+template <class OUT> struct FinishStore {
+    void *out;
+    const CeCoef *coef; // grad_x: the rows' units, else NULL
+    const float *top;   // grad_w: the largest unit
+    float inv_unit;     // 1 / ELEM::kUnit
+    int64_t sample;     // elements from one sample's output to the next
+    template <class ELEM, class S>
+    __device__ __forceinline__ void operator()(const Product &a, const Place &at, f32x4 (&acc)[S::SP][S::SQ]) const
+    {
+        const int p0 = at.p0 + at.wp * (S::SP * 16) + 4 * (at.lane >> 4);
+        const bool wide = a.p.rows % 4 == 0;
+#pragma unroll
+        for (int j = 0; j < S::SQ; ++j) {
+            const int q = at.q0 + at.wq * (S::SQ * 16) + j * 16 + (at.lane & 15);
+            if (q >= a.q.rows)
+                continue;
+            const float f = (coef ? coef[(int64_t)at.sample * a.q.rows + q].unit : *top) * inv_unit;
+            const int64_t to = at.sample * sample + (int64_t)q * a.p.rows;
+#pragma unroll
+            for (int k = 0; k < S::SP; ++k) {
+                const int p = p0 + k * 16;
+                if (wide) {
+                    if (p < a.p.rows)
+                        put4<OUT>(out, to + p, acc[k][j] * f);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (p + i < a.p.rows)
+                            put<OUT>(out, to + p + i, acc[k][j][i] * f);
+                }
+            }
+        }
+    }
+};
+
+// One part of a gradient's sum, in float32 [split][samples][q rows][ld]; added
+// to what an earlier piece left there.
+struct FinishPart {
+    float *part;
+    int64_t split, sample; // elements from one part, one sample to the next
+    int ld;                // p rows up to a multiple of 4
+    bool add;
+    template <class ELEM, class S>
+    __device__ __forceinline__ void operator()(const Product &a, const Place &at, f32x4 (&acc)[S::SP][S::SQ]) const
+    {
+        const int p0 = at.p0 + at.wp * (S::SP * 16) + 4 * (at.lane >> 4);
+#pragma unroll
+        for (int j = 0; j < S::SQ; ++j) {
+            const int q = at.q0 + at.wq * (S::SQ * 16) + j * 16 + (at.lane & 15);
+            if (q >= a.q.rows)
+                continue;
+            float *to = part + at.split * split + at.sample * sample + (int64_t)q * ld;
+#pragma unroll
+            for (int k = 0; k < S::SP; ++k) {
+                const int p = p0 + k * 16;
+                if (p < ld) {
+                    f32x4 v = acc[k][j];
+                    if (add)
+                        v += *(f32x4 *)(to + p);
+                    *(f32x4 *)(to + p) = v;
+                }
+            }
+        }
+    }
+};
+
+// ---------------------------------------------------------------------------
+// the kernels around the products
+// ---------------------------------------------------------------------------
+
+// Rows copied to dim_pad columns (zeros behind dim) and, where coef is given,
+// rows_pad rows a sample with every row times its unit over the largest one (a
+// power of two, so no rounding; zero for ignored rows, whatever they hold).
+template <class IN> __device__ __forceinline__ float get(const void *in, int64_t at) { return IN::to(((const uint16_t *)in)[at]); }
+template <> __device__ __forceinline__ float get<float>(const void *in, int64_t at) { return ((const float *)in)[at]; }
+
+template <class IN>
+__global__ __launch_bounds__(kBlock) void k_ce_pack(const void *in, uint16_t *out, int64_t plane, int rows, int rows_out,
+                                                    int dim, int dim_pad, int64_t n, const CeCoef *coef, const float *top)
+{
+    const int64_t i = ((int64_t)blockIdx.x * kBlock + threadIdx.x) * 4;
+    if (i >= n)
+        return;
+    const int64_t r = i / dim_pad;
+    const int d = (int)(i - r * dim_pad);
+    const int64_t sample = r / rows_out;
+    const int t = (int)(r - sample * rows_out);
+    float f = 1.0f;
+    bool keep = t < rows;
+    const int64_t row = sample * rows + t;
+    if (coef && keep) {
+        const CeCoef c = coef[row];
+        keep = c.fac != 0.0f;
+        f = c.unit / *top;
+    }
+    float v[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+        v[u] = keep && d + u < dim ? get<IN>(in, row * dim + d + u) * f : 0.0f;
+    if constexpr (std::is_same_v<IN, float>) {
+        const Planes a = planes_of(v[0]), b = planes_of(v[1]), c = planes_of(v[2]), e = planes_of(v[3]);
+        *(ushort4 *)(out + i) = make_ushort4(a.a, b.a, c.a, e.a);
+        *(ushort4 *)(out + plane + i) = make_ushort4(a.b, b.b, c.b, e.b);
+        *(ushort4 *)(out + 2 * plane + i) = make_ushort4(a.c, b.c, c.c, e.c);
+    } else {
+        *(ushort4 *)(out + i) = make_ushort4(IN::from(v[0]), IN::from(v[1]), IN::from(v[2]), IN::from(v[3]));
+    }
+}
+
+// Targets as int32: -1 ignored, -2 outside the classes.
+constexpr int kIgnored = -1, kOutside = -2;
+__device__ __forceinline__ int target_of(const void *target, bool t32, int64_t i, int64_t ignore, int classes)
+{
+    const int64_t t = t32 ? (int64_t)((const int32_t *)target)[i] : ((const int64_t *)target)[i];
+    return t == ignore ? kIgnored : t < 0 || t >= classes ? kOutside : (int)t;
+}
+__global__ __launch_bounds__(kBlock) void k_ce_targets(const void *target, bool t32, int64_t ignore, int classes,
+                                                       int32_t *out, int64_t n)
+{
+    const int64_t i = (int64_t)blockIdx.x * kBlock + threadIdx.x;
+    if (i < n)
+        out[i] = target_of(target, t32, i, ignore, classes);
+}
+
+// Joins a row's parts. A workgroup takes 16 rows, 16 threads a row: thread k
+// of a row takes parts k, k + 16, ...
+__global__ __launch_bounds__(kBlock) void k_ce_rows(const float2 *part, int parts, const float *picked,
+                                                    const int32_t *target, int64_t n, float z_weight, float *loss,
+                                                    CeRow *rows)
+{
+    __shared__ float2 sm[16][17];
+    const int r = threadIdx.x & 15, k0 = threadIdx.x >> 4;
+    const int64_t row = (int64_t)blockIdx.x * 16 + r;
+    float m = -kInf, sum = 0.0f;
+    if (row < n)
+        for (int k = k0; k < parts; k += 16) {
+            const float2 v = part[(int64_t)k * n + row];
+            const float top = fmaxf(m, v.x);
+            const float base = top == -kInf ? 0.0f : top;
+            sum = sum * __expf(m - base) + v.y * __expf(v.x - base);
+            m = top;
+        }
+    sm[k0][r] = make_float2(m, sum);
+    __syncthreads();
+    if (threadIdx.x >= 16 || row >= n)
+        return;
+    const int t = target[row];
+    const float z = t >= 0 ? picked[row] : -kInf;
+    float top = z;
+    for (int k = 0; k < 16; ++k)
+        top = fmaxf(top, sm[k][r].x);
+    const float base = top == -kInf ? 0.0f : top;
+    double others = 0.0;
+    for (int k = 0; k < 16; ++k)
+        others += (double)sm[k][r].y * (double)expf(sm[k][r].x - base);
+    const double mine = t >= 0 ? (double)expf(z - base) : 0.0;
+    const double total = others + mine;
+    const float lse = base + (float)log(total);
+    float l = mine > 0.5 ? (float)log1p(others / mine) : lse - z;
+    float miss = (float)(others / total);
+    l += z_weight != 0.0f ? z_weight * lse * lse : 0.0f;
+    if (t == kIgnored)
+        l = 0.0f;
+    if (t == kOutside)
+        l = miss = __builtin_nanf("");
+    loss[row] = l;
+    if (rows)
+        rows[row] = CeRow{top, (float)(1.0 / total), miss, lse};
+}
+
+// Sum (or mean over the rows that count) of the losses, in one workgroup in a
+// fixed order.
+__global__ __launch_bounds__(1024) void k_ce_total(const float *rows, const int32_t *target, int64_t n, int mean,
+                                                   float *loss, float *total)
+{
+    __shared__ double ssum[16];
+    __shared__ int scount[16];
+    double sum = 0.0;
+    int count = 0;
+    for (int64_t i = threadIdx.x; i < n; i += 1024) {
+        sum += (double)rows[i];
+        count += target[i] != kIgnored;
+    }
+    sum = wave_sum(sum);
+    for (int o = 32; o > 0; o >>= 1)
+        count += __shfl_xor(count, o);
+    if (lane_id() == 0) {
+        ssum[threadIdx.x >> 6] = sum;
+        scount[threadIdx.x >> 6] = count;
+    }
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        for (int w = 1; w < 16; ++w) {
+            sum += ssum[w];
+            count += scount[w];
+        }
+        loss[0] = (float)(mean ? sum / (double)max(count, 1) : sum);
+        if (total) {
+            total[0] = (float)sum;
+            total[1] = (float)max(count, 1);
+        }
+    }
+}
+
+// The backward pass's coefficients of a row. Its upstream gradient b and the
+// penalty's part c = 2 z_weight lse b are taken in units of a power of two at
+// least |b| + |c|, so that the stored gradient of the logits lies in [-1, 1].
+__global__ __launch_bounds__(kBlock) void k_ce_coef(const CeRow *rows, const int32_t *target, const float *grad_loss,
+                                                    const float *total, int reduction, float scale, float z_weight,
+                                                    float unit, int64_t n, CeCoef *coef, float *block_top)
+{
+    __shared__ float sm[kBlock / 64];
+    const int64_t i = (int64_t)blockIdx.x * kBlock + threadIdx.x;
+    float m = 0.0f;
+    if (i < n) {
+        const CeRow r = rows[i];
+        const int t = target[i];
+        float g = grad_loss[reduction == 0 ? i : 0];
+        if (reduction == 2)
+            g /= total[1];
+        const float b = g * scale;
+        const float c = z_weight != 0.0f ? 2.0f * z_weight * r.lse * b : 0.0f;
+        const float size = fabsf(b) + fabsf(c);
+        int e = 0;
+        if (size < kInf) // not NaN, not infinite
+            frexpf(size, &e);
+        e = min(max(e, -100), 100);
+        m = ldexpf(1.0f, e);
+        const float inv = ldexpf(1.0f, -e) * unit, mine = 1.0f - r.miss;
+        CeCoef k{r.top, (b + c) * inv * r.inv_total, (c * mine - b * r.miss) * inv, m};
+        if (t == kIgnored)
+            k.fac = k.at_target = m = 0.0f;
+        if (t == kOutside)
+            k.fac = __builtin_nanf("");
+        coef[i] = k;
+    }
+    for (int o = 32; o > 0; o >>= 1)
+        m = fmaxf(m, __shfl_xor(m, o));
+    if (lane_id() == 0)
+        sm[threadIdx.x >> 6] = m;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        for (int w = 1; w < kBlock / 64; ++w)
+            m = fmaxf(m, sm[w]);
+        block_top[blockIdx.x] = m;
+    }
+}
+
+__global__ __launch_bounds__(1024) void k_ce_top(const float *block_top, int n, float *top)
+{
+    __shared__ float sm[16];
+    float m = 0.0f;
+    for (int i = threadIdx.x; i < n; i += 1024)
+        m = fmaxf(m, block_top[i]);
+    for (int o = 32; o > 0; o >>= 1)
+        m = fmaxf(m, __shfl_xor(m, o));
+    if (lane_id() == 0)
+        sm[threadIdx.x >> 6] = m;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        for (int w = 1; w < 16; ++w)
+            m = fmaxf(m, sm[w]);
+        *top = m > 0.0f ? m : 1.0f; // every row ignored
+    }
+}
+
+// Adds up the parts of a gradient and rounds it.
+template <class OUT>
+__global__ __launch_bounds__(kBlock) void k_ce_join(const float *part, int splits, int64_t split, int cols, int ld,
+                                                    int64_t rows, const CeCoef *coef, const float *top, float inv_unit,
+                                                    void *out)
+{
+    const int64_t i = ((int64_t)blockIdx.x * kBlock + threadIdx.x) * 4;
+    const int64_t r = i / ld;
+    const int c = (int)(i - r * ld);
+    if (r >= rows)
+        return;
+    f32x4 v = *(const f32x4 *)(part + i);
+    for (int s = 1; s < splits; ++s)
+        v += *(const f32x4 *)(part + s * split + i);
+    v *= (coef ? coef[r].unit : *top) * inv_unit;
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+        if (c + u < cols)
+            put<OUT>(out, r * cols + c + u, v[u]);
+}
+
+// ---------------------------------------------------------------------------
+// host
+// ---------------------------------------------------------------------------
+
+using Large = Shape<256, 256, 2, 4, 2>;
+using Medium = Shape<128, 128, 2, 2, 2>;
+using Narrow = Shape<128, 16, 4, 1, 4>;
+
+int ceil_to(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
+int64_t pad_to(int64_t a, int64_t b) { return (a + b - 1) / b * b; }
+
+enum class Kind { large, medium, narrow };
+
+// The tile of a product of `classes` by `rows` results.
+Kind choose(int64_t p, int64_t q, int64_t batches, bool narrow_ok)
+{
+    if (narrow_ok && q <= 16)
+        return Kind::narrow;
+    if (ceil_to(p, 256) * (int64_t)ceil_to(q, 256) * batches >= 256)
+        return Kind::large;
+    return Kind::medium;
+}
+int tile_p(Kind k) { return k == Kind::large ? 256 : 128; }
+int tile_q(Kind k) { return k == Kind::large ? 256 : k == Kind::medium ? 128 : 16; }
+int waves_p(Kind k) { return k == Kind::narrow ? Narrow::WP : 2; }
+
+template <class ELEM, bool PLANES, bool PK, bool QK, class S, class F>
+void launch_shape(Product a, int64_t cover_p, int64_t cover_q, const F &f, hipStream_t s)
+{
+    a.tiles_p = ceil_to(cover_p, S::TP);
+    a.tiles_q = ceil_to(cover_q, S::TQ);
+    a.group = std::min(a.tiles_q, 8);
+    const void *k = (const void *)k_product<ELEM, PLANES, PK, QK, S, F>;
+    (void)set_dynamic_lds(k, S::lds);
+    const int64_t grid = (int64_t)a.tiles_p * a.tiles_q * a.samples * a.splits;
+    k_product<ELEM, PLANES, PK, QK, S, F><<<dim3((unsigned)grid), dim3(S::threads), S::lds, s>>>(a, f);
+}
+
+template <class ELEM, bool PLANES, bool PK, bool QK, class F>
+void launch_product(Kind kind, const Product &a, int64_t cover_p, int64_t cover_q, const F &f, hipStream_t s)
+{
+    if (kind == Kind::large)
+        launch_shape<ELEM, PLANES, PK, QK, Large>(a, cover_p, cover_q, f, s);
+    else if (kind == Kind::medium)
+        launch_shape<ELEM, PLANES, PK, QK, Medium>(a, cover_p, cover_q, f, s);
+    else if constexpr (!QK)
+        launch_shape<ELEM, PLANES, PK, QK, Narrow>(a, cover_p, cover_q, f, s);
+}
+
+struct Offsets {
+    size_t at = 0;
+    size_t take(size_t bytes)
+    {
+        const size_t o = at;
+        at += (std::max<size_t>(bytes, 16) + 255) & ~size_t(255);
+        return o;
+    }
+};
+
+bool aligned16(const void *p) { return ((uintptr_t)p & 15) == 0; }
+int planes(const CeProblem &p) { return p.type == ElemType::f32 ? 3 : 1; }
+int64_t all_rows(const CeProblem &p) { return (int64_t)p.samples * p.rows; }
+
+// x is copied where its rows are no whole steps (the copy's zeros are what ends
+// the sums), w only where its rows cannot be read 16 bytes at a time.
+void choose_packs(const CeProblem &p, bool *x, bool *w)
+{
+    *x = p.type == ElemType::f32 || p.dim % kCeStep || !aligned16(p.x);
+    *w = p.type == ElemType::f32 || p.dim % 8 || !aligned16(p.w);
+}
+
+template <class IN>
+void launch_pack(const void *in, uint16_t *out, int64_t samples, int rows, int rows_out, int dim, int dim_pad,
+                 const CeCoef *coef, const float *top, hipStream_t s)
+{
+    const int64_t n = samples * rows_out * dim_pad;
+    k_ce_pack<IN><<<dim3(blocks_for(n / 4, kBlock)), dim3(kBlock), 0, s>>>(in, out, n, rows, rows_out, dim, dim_pad, n,
+                                                                          coef, top);
+}
+
+// x, w as operands with the features contiguous.
+Operand features(const CeProblem &p, bool packed, const void *user, const uint16_t *copy, int64_t rows, int dim_pad)
+{
+    Operand o;
+    o.base = packed ? copy : (const uint16_t *)user;
+    o.ld = packed ? dim_pad : p.dim;
+    o.sample = rows * o.ld;
+    o.plane = p.samples * o.sample;
+    o.rows = (int)rows;
+    o.k = packed ? dim_pad : p.dim;
+    return o;
+}
+
+template <class F> void by_type(ElemType t, F f)
+{
+    if (t == ElemType::f32)
+        f(Bf16{}, std::true_type{}, float{});
+    else if (t == ElemType::bf16)
+        f(Bf16{}, std::false_type{}, Bf16{});
+    else
+        f(F16{}, std::false_type{}, F16{});
+}
+
+} // namespace
+
+CeForwardPlan ce_plan_forward(const CeProblem &p)
+{
+    CeForwardPlan f{};
+    choose_packs(p, &f.pack_x, &f.pack_w);
+    f.dim_pad = (int)pad_to(p.dim, kCeStep);
+    const Kind kind = choose(p.classes, p.rows, p.samples, true);
+    f.parts = ceil_to(p.classes, tile_p(kind)) * waves_p(kind);
+    const int64_t n = all_rows(p);
+    Offsets o;
+    f.x = o.take(f.pack_x ? n * f.dim_pad * 2 * planes(p) : 0);
+    f.w = o.take(f.pack_w ? (int64_t)p.samples * p.classes * f.dim_pad * 2 * planes(p) : 0);
+    f.target = o.take(n * sizeof(int32_t));
+    f.part = o.take((int64_t)f.parts * n * sizeof(float2));
+    f.picked = o.take(2 * n * sizeof(float));
+    f.bytes = o.at;
+    return f;
+}
+
+void ce_forward(const CeProblem &p, const CeForwardPlan &plan, uint8_t *ws, float *loss, CeRow *rows, float *total,
+                hipStream_t s)
+{
+    const int64_t n = all_rows(p);
+    auto *target = (int32_t *)(ws + plan.target);
+    auto *part = (float2 *)(ws + plan.part);
+    auto *picked = (float *)(ws + plan.picked);
+    float *row_loss = p.reduction == 0 ? loss : picked + n;
+    k_ce_targets<<<dim3(blocks_for(n, kBlock)), dim3(kBlock), 0, s>>>(p.target, p.target32, p.ignore_index, p.classes,
+                                                                     target, n);
+    auto *x = (uint16_t *)(ws + plan.x), *w = (uint16_t *)(ws + plan.w);
+    by_type(p.type, [&](auto elem, auto cut, auto io) {
+        using ELEM = decltype(elem);
+        using IO = decltype(io);
+        if (plan.pack_x)
+            launch_pack<IO>(p.x, x, p.samples, p.rows, p.rows, p.dim, plan.dim_pad, nullptr, nullptr, s);
+        if (plan.pack_w)
+            launch_pack<IO>(p.w, w, p.samples, p.classes, p.classes, p.dim, plan.dim_pad, nullptr, nullptr, s);
+        Product a{};
+        a.p = features(p, plan.pack_w, p.w, w, p.classes, plan.dim_pad);
+        a.q = features(p, plan.pack_x, p.x, x, p.rows, plan.dim_pad);
+        a.steps = plan.dim_pad / kCeStep;
+        a.samples = p.samples;
+        a.splits = 1;
+        launch_product<ELEM, decltype(cut)::value, false, false>(choose(p.classes, p.rows, p.samples, true), a,
+                                                                 p.classes, p.rows,
+                                                                 FinishStats{target, part, picked, p.scale}, s);
+    });
+    k_ce_rows<<<dim3(blocks_for(n, 16)), dim3(kBlock), 0, s>>>(part, plan.parts, picked, target, n, p.z_weight, row_loss,
+                                                              rows);
+    if (p.reduction != 0)
+        k_ce_total<<<dim3(1), dim3(1024), 0, s>>>(row_loss, target, n, p.reduction == 2, loss, total);
+}
+
+namespace {
+
+// The piece of the logits' gradient that exists at a time: what stays in the
+// 256 MB last-level cache between the product that writes it and the two that
+// read it.
+constexpr int64_t kPieceBytes = (int64_t)128 << 20;
+
+// Parts of a sum of `steps` steps so that a product of few tiles fills the card.
+int choose_splits(int64_t tiles, int64_t steps)
+{
+    if (tiles >= 256)
+        return 1;
+    return (int)std::max<int64_t>(1, std::min<int64_t>({512 / std::max<int64_t>(tiles, 1), steps / 8, 64}));
+}
+
+} // namespace
+
+CeBackwardPlan ce_plan_backward(const CeProblem &p, bool want_x, bool want_w)
+{
+    CeBackwardPlan b{};
+    choose_packs(p, &b.pack_x, &b.pack_w);
+    b.dim_pad = (int)pad_to(p.dim, kCeStep);
+    b.rows_pad = (int)pad_to(p.rows, kCeStep);
+    const int64_t n = all_rows(p), size = 2 * planes(p);
+    const int64_t whole = (int64_t)b.rows_pad * pad_to(p.classes, kCeStep) * size; // of one sample
+    if (whole <= kPieceBytes) {
+        b.piece_samples = (int)std::min<int64_t>(p.samples, kPieceBytes / whole);
+        b.piece_classes = p.classes;
+    } else {
+        b.piece_samples = 1;
+        const int64_t most = std::max<int64_t>(256, kPieceBytes / (b.rows_pad * size) / 256 * 256);
+        const int pieces = ceil_to(p.classes, most);
+        b.piece_classes = (int)std::min<int64_t>(p.classes, pad_to(ceil_to(p.classes, pieces), 256));
+    }
+    b.ld_g = (int)pad_to(b.piece_classes, kCeStep);
+    const Kind kx = choose(p.dim, p.rows, b.piece_samples, true), kw = choose(p.dim, b.piece_classes, b.piece_samples, false);
+    b.split_x = choose_splits((int64_t)ceil_to(p.dim, tile_p(kx)) * ceil_to(p.rows, tile_q(kx)) * b.piece_samples,
+                              b.ld_g / kCeStep);
+    b.split_w = choose_splits((int64_t)ceil_to(p.dim, tile_p(kw)) * ceil_to(b.piece_classes, tile_q(kw)) * b.piece_samples,
+                              b.rows_pad / kCeStep);
+    b.sum_x = b.split_x > 1 || b.piece_classes < p.classes;
+    const int64_t ld = pad_to(p.dim, 4);
+    Offsets o;
+    b.x = o.take(b.pack_x ? n * b.dim_pad * size : 0);
+    b.w = o.take(b.pack_w ? (int64_t)p.samples * p.classes * b.dim_pad * size : 0);
+    b.target = o.take(n * sizeof(int32_t));
+    b.coef = o.take(n * sizeof(CeCoef));
+    b.block_top = o.take(blocks_for(n, kBlock) * sizeof(float));
+    b.top = o.take(sizeof(float));
+    b.xs = o.take(want_w ? (int64_t)p.samples * b.rows_pad * b.dim_pad * size : 0);
+    b.g = o.take((int64_t)b.piece_samples * b.rows_pad * b.ld_g * size);
+    b.part_x = o.take(want_x && b.sum_x ? (int64_t)b.split_x * b.piece_samples * p.rows * ld * 4 : 0);
+    b.part_w = o.take(want_w && b.split_w > 1 ? (int64_t)b.split_w * b.piece_samples * b.piece_classes * ld * 4 : 0);
+    b.bytes = o.at;
+    return b;
+}
+
+void ce_backward(const CeProblem &p, const CeBackwardPlan &plan, uint8_t *ws, const CeRow *rows, const float *total,
+                 const float *grad_loss, void *grad_x, void *grad_w, hipStream_t s)
+{
+    const int64_t n = all_rows(p);
+    auto *target = (int32_t *)(ws + plan.target);
+    auto *coef = (CeCoef *)(ws + plan.coef);
+    auto *block_top = (float *)(ws + plan.block_top), *top = (float *)(ws + plan.top);
+    auto *x = (uint16_t *)(ws + plan.x), *w = (uint16_t *)(ws + plan.w);
+    auto *xs = (uint16_t *)(ws + plan.xs), *g = (uint16_t *)(ws + plan.g);
+    auto *part_x = (float *)(ws + plan.part_x), *part_w = (float *)(ws + plan.part_w);
+    const int64_t ld = pad_to(p.dim, 4);
+    k_ce_targets<<<dim3(blocks_for(n, kBlock)), dim3(kBlock), 0, s>>>(p.target, p.target32, p.ignore_index, p.classes,
+                                                                     target, n);
+    by_type(p.type, [&](auto elem, auto cut, auto io) {
+        using ELEM = decltype(elem);
+        using IO = decltype(io);
+        constexpr bool PLANES = decltype(cut)::value;
+        const float inv_unit = 1.0f / ELEM::kUnit;
+        const unsigned blocks = blocks_for(n, kBlock);
+        k_ce_coef<<<dim3(blocks), dim3(kBlock), 0, s>>>(rows, target, grad_loss, total, p.reduction, p.scale, p.z_weight,
+                                                        ELEM::kUnit, n, coef, block_top);
+        k_ce_top<<<dim3(1), dim3(1024), 0, s>>>(block_top, (int)blocks, top);
+        if (plan.pack_x)
+            launch_pack<IO>(p.x, x, p.samples, p.rows, p.rows, p.dim, plan.dim_pad, nullptr, nullptr, s);
+        if (plan.pack_w)
+            launch_pack<IO>(p.w, w, p.samples, p.classes, p.classes, p.dim, plan.dim_pad, nullptr, nullptr, s);
+        if (grad_w)
+            launch_pack<IO>(p.x, xs, p.samples, p.rows, plan.rows_pad, p.dim, plan.dim_pad, coef, top, s);
+        const Operand W = features(p, plan.pack_w, p.w, w, p.classes, plan.dim_pad);
+        const Operand X = features(p, plan.pack_x, p.x, x, p.rows, plan.dim_pad);
+        for (int s0 = 0; s0 < p.samples; s0 += plan.piece_samples) {
+            const int ns = std::min(plan.piece_samples, p.samples - s0);
+            for (int c0 = 0; c0 < p.classes; c0 += plan.piece_classes) {
+                const int nc = std::min(plan.piece_classes, p.classes - c0);
+                const int nc_pad = (int)pad_to(nc, kCeStep);
+                const int64_t plane_g = (int64_t)plan.piece_samples * plan.rows_pad * plan.ld_g;
+                { // the logits again, and their gradient
+                    Product a{};
+                    a.p = W;
+                    a.p.base += s0 * W.sample + (int64_t)c0 * W.ld;
+                    a.p.rows = nc;
+                    a.q = X;
+                    a.q.base += s0 * X.sample;
+                    a.steps = plan.dim_pad / kCeStep;
+                    a.samples = ns;
+                    a.splits = 1;
+                    const int64_t r0 = (int64_t)s0 * p.rows;
+                    launch_product<ELEM, PLANES, false, false>(
+                        choose(nc, p.rows, ns, true), a, nc_pad, plan.rows_pad,
+                        FinishGrad<PLANES>{target + r0, coef + r0, g, plane_g, p.scale, plan.rows_pad, plan.ld_g, c0}, s);
+                }
+                Operand G;
+                G.base = g;
+                G.sample = (int64_t)plan.rows_pad * plan.ld_g;
+                G.plane = plane_g;
+                G.ld = plan.ld_g;
+                if (grad_x) { // [rows][dim] = G [rows][classes] w [classes][dim]
+                    Product a{};
+                    a.p = W;
+                    a.p.base += s0 * W.sample + (int64_t)c0 * W.ld;
+                    a.p.rows = p.dim;
+                    a.p.k = nc;
+                    a.q = G;
+                    a.q.rows = p.rows;
+                    a.q.k = nc_pad;
+                    a.steps = nc_pad / kCeStep;
+                    a.samples = ns;
+                    const Kind kind = choose(p.dim, p.rows, plan.piece_samples, true);
+                    if (plan.sum_x) {
+                        a.splits = plan.split_x;
+                        const int64_t sample = (int64_t)p.rows * ld, split = plan.piece_samples * sample;
+                        launch_product<ELEM, PLANES, true, false>(kind, a, p.dim, p.rows,
+                                                                  FinishPart{part_x, split, sample, (int)ld, c0 > 0}, s);
+                    } else {
+                        a.splits = 1;
+                        const int64_t sample = (int64_t)p.rows * p.dim;
+                        launch_product<ELEM, PLANES, true, false>(
+                            kind, a, p.dim, p.rows,
+                            FinishStore<IO>{(uint8_t *)grad_x + s0 * sample * elem_size(p.type),
+                                            coef + (int64_t)s0 * p.rows, top, inv_unit, sample},
+                            s);
+                    }
+                }
+                if (grad_w) { // [classes][dim] = G^T [classes][rows] x [rows][dim]
+                    Product a{};
+                    a.p.base = xs + (int64_t)s0 * plan.rows_pad * plan.dim_pad;
+                    a.p.sample = (int64_t)plan.rows_pad * plan.dim_pad;
+                    a.p.plane = p.samples * a.p.sample;
+                    a.p.ld = plan.dim_pad;
+                    a.p.rows = p.dim;
+                    a.p.k = plan.rows_pad;
+                    a.q = G;
+                    a.q.rows = nc;
+                    a.q.k = plan.rows_pad;
+                    a.steps = plan.rows_pad / kCeStep;
+                    a.samples = ns;
+                    a.splits = plan.split_w;
+                    const Kind kind = choose(p.dim, plan.piece_classes, plan.piece_samples, false);
+                    const int64_t sample = (int64_t)p.classes * p.dim;
+                    void *to = (uint8_t *)grad_w + (s0 * sample + (int64_t)c0 * p.dim) * elem_size(p.type);
+                    if (plan.split_w > 1) {
+                        const int64_t per = (int64_t)nc * ld, split = ns * per;
+                        launch_product<ELEM, PLANES, true, true>(kind, a, p.dim, nc,
+                                                                 FinishPart{part_w, split, per, (int)ld, false}, s);
+                        // several samples only where a piece holds all their classes
+                        k_ce_join<IO><<<dim3(blocks_for(split / 4, kBlock)), dim3(kBlock), 0, s>>>(
+                            part_w, plan.split_w, split, p.dim, (int)ld, (int64_t)ns * nc, nullptr, top, inv_unit, to);
+                    } else {
+                        launch_product<ELEM, PLANES, true, true>(kind, a, p.dim, nc,
+                                                                 FinishStore<IO>{to, nullptr, top, inv_unit, sample}, s);
+                    }
+                }
+            }
+            if (grad_x && plan.sum_x) {
+                const int64_t sample = (int64_t)p.rows * ld, split = plan.piece_samples * sample;
+                k_ce_join<IO><<<dim3(blocks_for(ns * sample / 4, kBlock)), dim3(kBlock), 0, s>>>(
+                    part_x, plan.split_x, split, p.dim, (int)ld, (int64_t)ns * p.rows, coef + (int64_t)s0 * p.rows, top,
+                    inv_unit, (uint8_t *)grad_x + (int64_t)s0 * p.rows * p.dim * elem_size(p.type));
+            }
+        }
+    });
+}
+
+} // namespace apml

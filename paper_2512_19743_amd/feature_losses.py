@@ -1,0 +1,93 @@
+"""PyTorch autograd wrappers of the losses on features and on routed experts (computed in libapml)."""
+from __future__ import annotations
+
+from typing import Optional, Tuple
+
+import torch
+from torch.autograd.function import once_differentiable
+
+from . import _lib
+
+
+class LinearCEFunction(torch.autograd.Function):
+    """Softmax cross entropy against classes; the logits are computed again in backward, never kept."""
+
+    @staticmethod
+    def forward(ctx, x, w, target, keywords):
+        loss, state = _lib.apml_linear_ce_forward(x, w, target, keep_state=any(ctx.needs_input_grad[:2]), **keywords)
+        ctx.keywords = keywords
+        ctx.save_for_backward(x, w, target, state)
+        return loss
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, grad_loss):
+        x, w, target, state = ctx.saved_tensors
+        gx, gw = _lib.apml_linear_ce_backward(state, x, w, target, grad_loss.contiguous().to(torch.float32),
+                                              want_grad_x=ctx.needs_input_grad[0], want_grad_w=ctx.needs_input_grad[1],
+                                              **ctx.keywords)
+        return gx, gw, None, None
+
+
+def linear_ce_loss(x: torch.Tensor, w: torch.Tensor, target: torch.Tensor, *, scale: float = 1.0,
+                   z_weight: float = 0.0, ignore_index: int = -100, reduction: str = "mean") -> torch.Tensor:
+    """Softmax cross entropy of the rows of x against the classes w, without storing the logits
+    scale * x @ w.T; float32, with gradients for x and w in their own type.
+
+    x (..., dim) and w (classes, dim): one set of classes, a code book or a vocabulary. x (B, N, dim) and
+    w (B, M, dim): each sample with its own, as when the descriptors of one cloud's points are matched to
+    those of the other's (scale: 1 / temperature). float32, bfloat16 or float16 GPU tensors.
+    target: the rows' classes, int64 or int32, of x's leading shape; ignore_index: a row that adds nothing.
+    z_weight: weight of the squared log-sum-exp that is added per row.
+    reduction: 'none' (target's shape), 'sum', or 'mean' over the rows that are not ignored.
+    """
+    keywords = dict(scale=scale, z_weight=z_weight, ignore_index=ignore_index, reduction=reduction)
+    return LinearCEFunction.apply(x.contiguous(), w.contiguous(), target.contiguous(), keywords)
+
+
+class BalanceFunction(torch.autograd.Function):
+    """Balance loss of routed experts and the tokens per expert; the softmax is computed again in backward."""
+
+    @staticmethod
+    def forward(ctx, logits, experts, counts, valid, z_weight, reduction):
+        loss, got, state = _lib.apml_balance_forward(logits, experts, counts=counts, valid=valid, z_weight=z_weight,
+                                                     reduction=reduction, keep_state=ctx.needs_input_grad[0])
+        ctx.z_weight, ctx.reduction = z_weight, reduction
+        ctx.save_for_backward(logits, valid, state)
+        if counts is not None:  # an input is no output
+            got = torch.empty(0, dtype=torch.int64, device=logits.device)
+        ctx.mark_non_differentiable(got)
+        return loss, got
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, grad_loss, _):
+        logits, valid, state = ctx.saved_tensors
+        grad = _lib.apml_balance_backward(state, logits, grad_loss.contiguous().to(torch.float32), valid=valid,
+                                          z_weight=ctx.z_weight, reduction=ctx.reduction)
+        return grad, None, None, None, None, None
+
+
+def balance_loss(logits: torch.Tensor, experts: Optional[torch.Tensor] = None, *, counts: Optional[torch.Tensor] = None,
+                 valid: Optional[torch.Tensor] = None, z_weight: float = 0.0, reduction: str = "mean"
+                 ) -> Tuple[torch.Tensor, torch.Tensor]:
+    """(loss, counts): E sum_e f_e P_e per sample, with f_e the share of expert e in the chosen experts and
+    P_e the mean of its softmax probability over the valid tokens, plus z_weight times the mean squared
+    log-sum-exp; and the tokens per expert, int64.
+
+    logits (B, tokens, experts), a loss per sample, or (tokens, experts), one sample; float32, bfloat16 or
+    float16 GPU tensors. experts (..., chosen): the experts that each token goes to, int64 or int32, -1 for
+    a dropped slot. counts instead: the tokens per expert, (B, experts) or (experts,), for instance the sum
+    of every rank's expert_counts. valid: bool, the tokens' shape, False for padding.
+    The gradient flows into logits through the probabilities, not through the counts.
+    reduction: 'none' (per sample), 'sum' or 'mean' over the samples.
+    """
+    c = lambda t: t.contiguous() if t is not None else None  # noqa: E731
+    loss, got = BalanceFunction.apply(logits.contiguous(), c(experts), c(counts), c(valid), z_weight, reduction)
+    return loss, (counts if counts is not None else got)
+
+
+def expert_counts(experts: torch.Tensor, num_experts: int, *, valid: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Tokens per expert, int64 (B, num_experts) or (num_experts,), of experts (B, tokens, chosen) or
+    (tokens, chosen); entries outside [0, num_experts) are dropped slots, tokens that are not valid padding."""
+    return _lib.apml_expert_counts(experts.contiguous(), num_experts, valid=valid.contiguous() if valid is not None else None)
