@@ -15,9 +15,10 @@ inline size_t elem_size(ElemType t) { return t == ElemType::f32 ? 4 : 2; }
 
 constexpr int kCeStep = 64; // elements of the summed axis that one step of a product takes
 
-// What the forward pass keeps of a row: its largest logit, 1 / sum exp(z - top),
-// the part of its softmax that is not the target's, and its log-sum-exp. The
-// loss and the target's gradient come from `miss`, a sum without the target's
+// What the forward pass keeps of a row: its largest logit in units of log 2,
+// 1 / sum exp(z - top),
+// the part of its softmax that is not the target's, and its
+// log-sum-exp. The loss and the target's gradient come from `miss`, a sum without the target's
 // term: where the target's probability is next to 1, lse - z_target and p - 1
 // would be differences of nearly equal numbers.
 struct CeRow {
@@ -40,7 +41,7 @@ struct CeForwardPlan {
     bool pack_x, pack_w;         // copied: rows of dim_pad elements, in planes for float32
     int dim_pad;                 // dim up to a multiple of kCeStep
     int parts;                   // groups of classes with a maximum and a sum of their own
-    size_t x, w, target, part, picked, bytes;
+    size_t x, w, part, picked, sums, ticket, bytes;
 };
 CeForwardPlan ce_plan_forward(const CeProblem &p);
 // loss: [samples * rows] (reduction none) or [1]; rows: the state or NULL;
@@ -55,7 +56,8 @@ struct CeBackwardPlan {
     int ld_g;                    // its columns, a multiple of kCeStep
     int split_x, split_w;        // parts of the sum over the classes (grad_x) and over the rows (grad_w)
     bool sum_x;                  // grad_x is summed in float32 over several pieces or parts
-    size_t x, w, target, coef, block_top, top, xs, g, part_x, part_w, bytes;
+    int tops;                    // workgroups of the pass over the upstream gradients (0: all rows have the same)
+    size_t x, w, coef, block_top, top, xs, g, part_x, part_w, bytes;
 };
 CeBackwardPlan ce_plan_backward(const CeProblem &p, bool want_x, bool want_w);
 void ce_backward(const CeProblem &p, const CeBackwardPlan &plan, uint8_t *ws, const CeRow *rows, const float *total,

@@ -17,6 +17,8 @@
 // below 2^-23 of a term). bfloat16 matrix instructions run at 16 times the rate
 // of float32 ones, so six of them cost 3/8 of one float32 product.
 #include <algorithm>
+#include <cfloat>
+#include <cmath>
 
 #include "apml_internal.h"
 #include "device_common.h"
@@ -33,6 +35,22 @@ typedef short i16x4 __attribute__((ext_vector_type(4)));
 typedef short i16x8 __attribute__((ext_vector_type(8)));
 
 using lds_char = __attribute__((address_space(3))) char;
+
+constexpr float kLog2E = 1.44269504088896340736f;
+
+// The rows' targets as the caller holds them.
+constexpr int kIgnored = -1, kOutside = -2;
+struct Targets {
+    const void *at;
+    bool is32;
+    int classes;
+    int64_t ignore;
+    __device__ __forceinline__ int operator[](int64_t i) const
+    {
+        const int64_t t = is32 ? (int64_t)((const int32_t *)at)[i] : ((const int64_t *)at)[i];
+        return t == ignore ? kIgnored : t < 0 || t >= classes ? kOutside : (int)t;
+    }
+};
 
 // ---------------------------------------------------------------------------
 // 16-bit elements
@@ -110,21 +128,23 @@ __device__ __forceinline__ int k_swizzle(int k) { return ((k & 3) | ((k >> 1) & 
 // Byte offset, from the operand's base of a step, of what lane `lane` of load
 // `j` (1 KB of the tile) fetches. With k contiguous the tile holds ROWS rows of
 // 8 chunks of 16 bytes, chunk c of row r in slot c ^ (r & 7): the 16 rows that a
-// fragment read touches then lie in different banks. With the rows contiguous
-// it holds kCeStep rows of ROWS / 8 chunks, moved by k_swizzle for the same
-// reason (a transposing read touches the same columns of 16 rows).
+// fragment read touches then lie in different banks (EIGHTS: the rows that
+// p_fragment touches). With the rows contiguous it holds kCeStep rows of ROWS / 8
+// chunks, moved by k_swizzle for the same reason (a transposing read touches the
+// same columns of 16 rows).
 // The base is that of row first_row (a tile of the padded rows may begin behind
 // the last one).
 template <bool KS> __device__ __forceinline__ int first_row(const Operand &o, int r0)
 {
     return min(r0, KS ? (o.rows - 1) & ~7 : o.rows - 1);
 }
-template <int ROWS, bool KS>
+template <bool EIGHTS> __device__ __forceinline__ int row_swizzle(int r) { return EIGHTS ? (r & 3) | ((r >> 1) & 4) : r & 7; }
+template <int ROWS, bool KS, bool EIGHTS>
 __device__ __forceinline__ uint32_t tile_offset(const Operand &o, int r0, int j, int lane, int k_left)
 {
     if constexpr (!KS) {
         const int r = j * 8 + (lane >> 3);
-        const int c = (lane & 7) ^ (r & 7);
+        const int c = (lane & 7) ^ row_swizzle<EIGHTS>(r);
         const int row = min(r0 + r, o.rows - 1);
         return (uint32_t)((row - first_row<KS>(o, r0)) * o.ld + min(c, (k_left - 1) >> 3) * 8) * 2u;
     } else {
@@ -166,14 +186,18 @@ __device__ __forceinline__ void wait_lds_and_meet()
 }
 
 // The 16 x 32 fragment of a tile at rows r .. r + 15 and elements 32 h ..:
-// lane l holds row l & 15, elements 8 (l >> 4) .. + 7.
-template <int ROWS, bool KS> __device__ __forceinline__ i16x8 fragment(const lds_char *tile, int r, int h, int lane)
+// lane l holds row l & 15, elements 8 (l >> 4) .. + 7. EIGHTS: fragment `i` of
+// 32 rows holds rows 8 a + 4 (i & 1) .. + 3 for a = 0 .. 3, so that in the
+// results a lane's values of two neighbouring fragments are 8 neighbours.
+template <int ROWS, bool KS, bool EIGHTS>
+__device__ __forceinline__ i16x8 fragment(const lds_char *tile, int r0, int i, int h, int lane)
 {
     if constexpr (!KS) {
-        const int row = r + (lane & 15);
-        const int slot = (h * 4 + (lane >> 4)) ^ (row & 7);
+        const int row = EIGHTS ? r0 + (i >> 1) * 32 + ((lane & 12) << 1) + (i & 1) * 4 + (lane & 3) : r0 + i * 16 + (lane & 15);
+        const int slot = (h * 4 + (lane >> 4)) ^ row_swizzle<EIGHTS>(row);
         return *(const __attribute__((address_space(3))) i16x8 *)(tile + row * 128 + slot * 16);
     } else {
+        const int r = r0 + i * 16;
         // a transposing read gives lane i of 16 the column i of 4 rows of 16
         const int k = h * 32 + (lane >> 4) * 8 + ((lane & 15) >> 2);
         const int col = r + (lane & 3) * 4;
@@ -240,10 +264,10 @@ __global__ __launch_bounds__(S::threads) void k_product(Product a, Finish finish
         const int kp = min(kCeStep, a.p.k - step * kCeStep), kq = min(kCeStep, a.q.k - step * kCeStep);
 #pragma unroll
         for (int j = 0; j < S::LP; ++j)
-            op[j] = tile_offset<S::TP, PK>(a.p, at.p0, wave * S::LP + j, lane, kp);
+            op[j] = tile_offset<S::TP, PK, !PK>(a.p, at.p0, wave * S::LP + j, lane, kp);
 #pragma unroll
         for (int j = 0; j < S::LQ; ++j)
-            oq[j] = tile_offset<S::TQ, QK>(a.q, at.q0, (wave * S::LQ + j) % (S::TQ / 8), lane, kq);
+            oq[j] = tile_offset<S::TQ, QK, false>(a.q, at.q0, (wave * S::LQ + j) % (S::TQ / 8), lane, kq);
     };
     const int64_t step_p = PK ? kCeStep * a.p.ld : kCeStep, step_q = QK ? kCeStep * a.q.ld : kCeStep;
     const uint64_t base_p = (uint64_t)(a.p.base + at.sample * a.p.sample + first_row<PK>(a.p, at.p0) * (PK ? 1 : a.p.ld));
@@ -296,10 +320,10 @@ __global__ __launch_bounds__(S::threads) void k_product(Product a, Finish finish
             i16x8 fp[S::SP], fq[S::SQ];
 #pragma unroll
             for (int j = 0; j < S::SQ; ++j)
-                fq[j] = fragment<S::TQ, QK>(tq, at.wq * (S::SQ * 16) + j * 16, h, lane);
+                fq[j] = fragment<S::TQ, QK, false>(tq, at.wq * (S::SQ * 16), j, h, lane);
 #pragma unroll
             for (int k = 0; k < S::SP; ++k)
-                fp[k] = fragment<S::TP, PK>(tp, at.wp * (S::SP * 16) + k * 16, h, lane);
+                fp[k] = fragment<S::TP, PK, !PK>(tp, at.wp * (S::SP * 16), k, h, lane);
 #pragma unroll
             for (int k = 0; k < S::SP; ++k)
 #pragma unroll
@@ -307,68 +331,103 @@ __global__ __launch_bounds__(S::threads) void k_product(Product a, Finish finish
                     acc[k][j] = ELEM::mma(fp[k], fq[j], acc[k][j]);
         }
     }
-    // lane l holds, of 16 x 16 results, q = l & 15 and p = 4 (l >> 4) .. + 3
+    // lane l holds, of 16 x 16 results, q = l & 15 and p = 4 (l >> 4) .. + 3; with
+    // P's k contiguous, of 32 x 16, p = 8 (l >> 4) .. + 7 in two neighbours acc
     finish.template operator()<ELEM, S>(a, at, acc);
 }
 
 // --- what becomes of the results -------------------------------------------
 
 // Forward: per row (q) the maximum and the sum of exp(z - max) over a wave's
-// classes (p), without the target's, whose logit is kept apart.
+// classes (p), without the target's, whose logit is kept apart. Logits are in
+// units of log 2 from here on (exp2 is the instruction): z = acc * scale2. Per
+// logit a maximum, a multiply-add, an exponential and a sum; which class is a
+// row's target is asked only in waves whose classes hold one, which classes are
+// there at all only in the last tile.
 struct FinishStats {
-    const int32_t *target; // [samples * rows], below 0 where there is none
-    float2 *part;          // [parts][samples * rows]
-    float *picked;         // [samples * rows]
-    float scale;
+    Targets target; // [samples * rows]
+    float2 *part;   // [parts][samples * rows]
+    float *picked;  // [samples * rows]
+    int *ticket;    // cleared for k_ce_rows
+    float scale2;
     template <class ELEM, class S>
     __device__ __forceinline__ void operator()(const Product &a, const Place &at, f32x4 (&acc)[S::SP][S::SQ]) const
     {
+        if (blockIdx.x == 0 && threadIdx.x == 0)
+            *ticket = 0;
+        if (scale2 >= 0.0f)
+            reduce<S, true>(a, at, acc);
+        else
+            reduce<S, false>(a, at, acc);
+    }
+    template <class S, bool POSITIVE>
+    __device__ __forceinline__ void reduce(const Product &a, const Place &at, f32x4 (&acc)[S::SP][S::SQ]) const
+    {
+        constexpr float none = POSITIVE ? -kInf : kInf;
+        const auto further = [](float x, float y) { return POSITIVE ? fmaxf(x, y) : fminf(x, y); };
         const int g = at.lane >> 4;
-        const int v0 = at.p0 + at.wp * (S::SP * 16) + 4 * g;
+        const int w0 = at.p0 + at.wp * (S::SP * 16), v0 = w0 + 8 * g;
         const int64_t total = (int64_t)a.samples * a.q.rows;
+        if (w0 + S::SP * 16 > a.p.rows) {
+#pragma unroll
+            for (int k = 0; k < S::SP; ++k)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (v0 + (k >> 1) * 32 + (k & 1) * 4 + i >= a.p.rows)
+#pragma unroll
+                        for (int j = 0; j < S::SQ; ++j)
+                            acc[k][j][i] = none;
+        }
 #pragma unroll
         for (int j = 0; j < S::SQ; ++j) {
             const int t = at.q0 + at.wq * (S::SQ * 16) + j * 16 + (at.lane & 15);
             const int64_t row = (int64_t)at.sample * a.q.rows + t;
             const bool in = t < a.q.rows;
-            const int target = in ? target_at(row) : -1;
-            float m = -kInf;
+            const int d = (in ? target[row] : kIgnored) - v0;
+            if (__any(d >= 0 && d < S::SP * 16)) {
+#pragma unroll
+                for (int k = 0; k < S::SP; ++k)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (d == (k >> 1) * 32 + (k & 1) * 4 + i) {
+                            picked[row] = acc[k][j][i] * scale2;
+                            acc[k][j][i] = none;
+                        }
+            }
+            float m = none;
 #pragma unroll
             for (int k = 0; k < S::SP; ++k)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int v = v0 + k * 16 + i;
-                    float z = acc[k][j][i] * scale;
-                    if (v == target)
-                        picked[row] = z;
-                    if (v == target || v >= a.p.rows)
-                        z = -kInf;
-                    acc[k][j][i] = z;
-                    m = fmaxf(m, z);
-                }
-            m = fmaxf(m, __shfl_xor(m, 16));
-            m = fmaxf(m, __shfl_xor(m, 32));
-            const float base = m == -kInf ? 0.0f : m;
+                for (int i = 0; i < 4; ++i)
+                    m = further(m, acc[k][j][i]);
+            m = further(m, __shfl_xor(m, 16));
+            m = further(m, __shfl_xor(m, 32));
+            const float top = m == none ? -kInf : m * scale2;
+            const float base = top == -kInf ? 0.0f : top;
             float sum = 0.0f;
 #pragma unroll
             for (int k = 0; k < S::SP; ++k)
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
-                    sum += __expf(acc[k][j][i] - base);
+                    sum += __builtin_amdgcn_exp2f(__builtin_fmaf(acc[k][j][i], scale2, -base));
             sum += __shfl_xor(sum, 16);
             sum += __shfl_xor(sum, 32);
             if (in && g == 0)
-                part[(int64_t)(at.p0 / S::TP * S::WP + at.wp) * total + row] = make_float2(m, sum);
+                part[(int64_t)(at.p0 / S::TP * S::WP + at.wp) * total + row] = make_float2(top, sum);
         }
     }
-    __device__ __forceinline__ int target_at(int64_t row) const { return target[row]; }
 };
 
 // What the backward pass needs of a row: the logits' gradient is
-// fac exp(z - top), or at_target for the target's class, in units of the row's
-// power of two (unit); fac 0: an ignored row.
+// fac exp2(z - top), or at_target for the target's class, in units of `unit`;
+// fac 0: an ignored row.
 struct CeCoef {
     float top, fac, at_target, unit;
+};
+// The units' common part, and the largest unit: every unit is the first times a
+// power of two.
+struct CeTop {
+    float unit, top;
 };
 
 // Backward: the logits' gradient of a piece, rounded to the operands' type (the
@@ -376,50 +435,79 @@ struct CeCoef {
 // its own size at most, as the operands x and w themselves are), or in three
 // planes for float32.
 template <bool PLANES> struct FinishGrad {
-    const int32_t *target;
+    Targets target;
     const CeCoef *coef;
+    int64_t row0;        // the piece's first row
     uint16_t *g;         // [samples of the piece][rows_pad][ld]
     int64_t plane;
-    float scale;
+    float scale2;
     int rows_pad, ld, class0;
     template <class ELEM, class S>
     __device__ __forceinline__ void operator()(const Product &a, const Place &at, f32x4 (&acc)[S::SP][S::SQ]) const
     {
-        const int c0 = at.p0 + at.wp * (S::SP * 16) + 4 * (at.lane >> 4);
+        const int w0 = at.p0 + at.wp * (S::SP * 16), v0 = w0 + 8 * (at.lane >> 4);
+        const bool edge = w0 + S::SP * 16 > a.p.rows;
 #pragma unroll
         for (int j = 0; j < S::SQ; ++j) {
             const int t = at.q0 + at.wq * (S::SQ * 16) + j * 16 + (at.lane & 15);
-            if (t >= rows_pad)
-                continue;
-            const int64_t row = (int64_t)at.sample * a.q.rows + t;
+            const int64_t row = row0 + (int64_t)at.sample * a.q.rows + t;
             CeCoef c{0.0f, 0.0f, 0.0f, 0.0f};
-            int target = -1;
+            int d = kIgnored;
             if (t < a.q.rows) {
                 c = coef[row];
-                target = this->target[row] - class0;
+                d = target[row] - class0 - v0;
+            }
+            if (__any(c.fac == 0.0f)) {
+#pragma unroll
+                for (int k = 0; k < S::SP; ++k)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        acc[k][j][i] = c.fac == 0.0f ? 0.0f : acc[k][j][i];
             }
 #pragma unroll
-            for (int k = 0; k < S::SP; ++k) {
-                const int v = c0 + k * 16;
-                if (v >= ld)
-                    continue;
-                float d[4];
+            for (int k = 0; k < S::SP; ++k)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const float e = __expf(acc[k][j][i] * scale - c.top);
-                    d[i] = v + i == target ? c.at_target : c.fac * e;
-                    if (c.fac == 0.0f || v + i >= a.p.rows)
-                        d[i] = 0.0f;
-                }
-                uint16_t *to = g + ((int64_t)at.sample * rows_pad + t) * ld + v;
+                for (int i = 0; i < 4; ++i)
+                    acc[k][j][i] = c.fac * __builtin_amdgcn_exp2f(__builtin_fmaf(acc[k][j][i], scale2, -c.top));
+            if (__any(d >= 0 && d < S::SP * 16)) {
+#pragma unroll
+                for (int k = 0; k < S::SP; ++k)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (d == (k >> 1) * 32 + (k & 1) * 4 + i)
+                            acc[k][j][i] = c.at_target;
+            }
+            if (edge) {
+#pragma unroll
+                for (int k = 0; k < S::SP; ++k)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (v0 + (k >> 1) * 32 + (k & 1) * 4 + i >= a.p.rows)
+                            acc[k][j][i] = 0.0f;
+            }
+            uint16_t *to = g + ((int64_t)at.sample * rows_pad + t) * ld + v0;
+#pragma unroll
+            for (int k = 0; k < S::SP; k += 2) {
+                if (t >= rows_pad || v0 + k * 16 >= ld)
+                    continue;
+                i16x8 p0;
                 if constexpr (PLANES) {
-                    const Planes x = planes_of(d[0]), y = planes_of(d[1]), z = planes_of(d[2]), u = planes_of(d[3]);
-                    *(ushort4 *)to = make_ushort4(x.a, y.a, z.a, u.a);
-                    *(ushort4 *)(to + plane) = make_ushort4(x.b, y.b, z.b, u.b);
-                    *(ushort4 *)(to + 2 * plane) = make_ushort4(x.c, y.c, z.c, u.c);
+                    i16x8 p1, p2;
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const Planes x = planes_of(acc[k + (i >> 2)][j][i & 3]);
+                        p0[i] = (short)x.a;
+                        p1[i] = (short)x.b;
+                        p2[i] = (short)x.c;
+                    }
+                    *(i16x8 *)(to + plane + k * 16) = p1;
+                    *(i16x8 *)(to + 2 * plane + k * 16) = p2;
                 } else {
-                    *(ushort4 *)to = make_ushort4(ELEM::from(d[0]), ELEM::from(d[1]), ELEM::from(d[2]), ELEM::from(d[3]));
+#pragma unroll
+                    for (int i = 0; i < 8; ++i)
+                        p0[i] = (short)ELEM::from(acc[k + (i >> 2)][j][i & 3]);
                 }
+                *(i16x8 *)(to + k * 16) = p0;
             }
         }
     }
@@ -443,7 +531,7 @@ template <> __device__ __forceinline__ void put4<float>(void *out, int64_t at, f
 template <class OUT> struct FinishStore {
     void *out;
     const CeCoef *coef; // grad_x: the rows' units, else NULL
-    const float *top;   // grad_w: the largest unit
+    const CeTop *top;   // grad_w: the largest unit
     float inv_unit;     // 1 / ELEM::kUnit
     int64_t sample;     // elements from one sample's output to the next
     template <class ELEM, class S>
@@ -456,7 +544,7 @@ template <class OUT> struct FinishStore {
             const int q = at.q0 + at.wq * (S::SQ * 16) + j * 16 + (at.lane & 15);
             if (q >= a.q.rows)
                 continue;
-            const float f = (coef ? coef[(int64_t)at.sample * a.q.rows + q].unit : *top) * inv_unit;
+            const float f = (coef ? coef[(int64_t)at.sample * a.q.rows + q].unit : top->top) * inv_unit;
             const int64_t to = at.sample * sample + (int64_t)q * a.p.rows;
 #pragma unroll
             for (int k = 0; k < S::SP; ++k) {
@@ -511,205 +599,331 @@ struct FinishPart {
 // ---------------------------------------------------------------------------
 
 // Rows copied to dim_pad columns (zeros behind dim) and, where coef is given,
-// rows_pad rows a sample with every row times its unit over the largest one (a
+// rows_out rows a sample with every row times its unit over the largest one (a
 // power of two, so no rounding; zero for ignored rows, whatever they hold).
 template <class IN> __device__ __forceinline__ float get(const void *in, int64_t at) { return IN::to(((const uint16_t *)in)[at]); }
 template <> __device__ __forceinline__ float get<float>(const void *in, int64_t at) { return ((const float *)in)[at]; }
 
-template <class IN>
-__global__ __launch_bounds__(kBlock) void k_ce_pack(const void *in, uint16_t *out, int64_t plane, int rows, int rows_out,
-                                                    int dim, int dim_pad, int64_t n, const CeCoef *coef, const float *top)
+struct PackJob {
+    const void *in;
+    uint16_t *out;
+    int64_t n;           // elements of one plane of out
+    int rows, rows_out;  // per sample
+    const CeCoef *coef;
+    unsigned blocks;
+};
+constexpr int kPackJobs = 3;
+struct PackJobs {
+    PackJob job[kPackJobs];
+    int dim, dim_pad;
+    const CeTop *top;
+};
+
+template <class IN> __global__ __launch_bounds__(kBlock) void k_ce_pack(PackJobs jobs)
 {
-    const int64_t i = ((int64_t)blockIdx.x * kBlock + threadIdx.x) * 4;
-    if (i >= n)
+    unsigned block = blockIdx.x;
+    int which = 0;
+    while (block >= jobs.job[which].blocks)
+        block -= jobs.job[which++].blocks;
+    const PackJob &p = jobs.job[which];
+    const int64_t i = ((int64_t)block * kBlock + threadIdx.x) * 8;
+    if (i >= p.n)
         return;
-    const int64_t r = i / dim_pad;
-    const int d = (int)(i - r * dim_pad);
-    const int64_t sample = r / rows_out;
-    const int t = (int)(r - sample * rows_out);
+    const int64_t r = i / jobs.dim_pad;
+    const int d = (int)(i - r * jobs.dim_pad);
+    const int64_t sample = r / p.rows_out;
+    const int t = (int)(r - sample * p.rows_out);
     float f = 1.0f;
-    bool keep = t < rows;
-    const int64_t row = sample * rows + t;
-    if (coef && keep) {
-        const CeCoef c = coef[row];
+    bool keep = t < p.rows;
+    const int64_t row = sample * p.rows + t;
+    if (p.coef && keep) {
+        const CeCoef c = p.coef[row];
         keep = c.fac != 0.0f;
-        f = c.unit / *top;
+        f = c.unit / jobs.top->top;
     }
-    float v[4];
+    float v[8];
+    const int64_t at = row * jobs.dim + d;
+    constexpr int size = std::is_same_v<IN, float> ? 4 : 2;
+    if (keep && d + 8 <= jobs.dim && (((uintptr_t)p.in + at * size) & 15) == 0) {
+        if constexpr (size == 4) {
+            const f32x4 lo = ((const f32x4 *)((const float *)p.in + at))[0], hi = ((const f32x4 *)((const float *)p.in + at))[1];
 #pragma unroll
-    for (int u = 0; u < 4; ++u)
-        v[u] = keep && d + u < dim ? get<IN>(in, row * dim + d + u) * f : 0.0f;
-    if constexpr (std::is_same_v<IN, float>) {
-        const Planes a = planes_of(v[0]), b = planes_of(v[1]), c = planes_of(v[2]), e = planes_of(v[3]);
-        *(ushort4 *)(out + i) = make_ushort4(a.a, b.a, c.a, e.a);
-        *(ushort4 *)(out + plane + i) = make_ushort4(a.b, b.b, c.b, e.b);
-        *(ushort4 *)(out + 2 * plane + i) = make_ushort4(a.c, b.c, c.c, e.c);
+            for (int u = 0; u < 4; ++u) {
+                v[u] = lo[u] * f;
+                v[u + 4] = hi[u] * f;
+            }
+        } else {
+            const i16x8 raw = *(const i16x8 *)((const uint16_t *)p.in + at);
+#pragma unroll
+            for (int u = 0; u < 8; ++u)
+                v[u] = IN::to((uint16_t)raw[u]) * f;
+        }
     } else {
-        *(ushort4 *)(out + i) = make_ushort4(IN::from(v[0]), IN::from(v[1]), IN::from(v[2]), IN::from(v[3]));
+#pragma unroll
+        for (int u = 0; u < 8; ++u)
+            v[u] = keep && d + u < jobs.dim ? get<IN>(p.in, at + u) * f : 0.0f;
     }
+    i16x8 p0;
+    if constexpr (size == 4) {
+        i16x8 p1, p2;
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+            const Planes x = planes_of(v[u]);
+            p0[u] = (short)x.a;
+            p1[u] = (short)x.b;
+            p2[u] = (short)x.c;
+        }
+        *(i16x8 *)(p.out + p.n + i) = p1;
+        *(i16x8 *)(p.out + 2 * p.n + i) = p2;
+    } else {
+#pragma unroll
+        for (int u = 0; u < 8; ++u)
+            p0[u] = (short)IN::from(v[u]);
+    }
+    *(i16x8 *)(p.out + i) = p0;
 }
 
-// Targets as int32: -1 ignored, -2 outside the classes.
-constexpr int kIgnored = -1, kOutside = -2;
-__device__ __forceinline__ int target_of(const void *target, bool t32, int64_t i, int64_t ignore, int classes)
-{
-    const int64_t t = t32 ? (int64_t)((const int32_t *)target)[i] : ((const int64_t *)target)[i];
-    return t == ignore ? kIgnored : t < 0 || t >= classes ? kOutside : (int)t;
-}
-__global__ __launch_bounds__(kBlock) void k_ce_targets(const void *target, bool t32, int64_t ignore, int classes,
-                                                       int32_t *out, int64_t n)
-{
-    const int64_t i = (int64_t)blockIdx.x * kBlock + threadIdx.x;
-    if (i < n)
-        out[i] = target_of(target, t32, i, ignore, classes);
-}
+// What the workgroups of k_ce_rows leave for the last of them.
+struct LossSum {
+    double sum;
+    int64_t count;
+};
 
-// Joins a row's parts. A workgroup takes 16 rows, 16 threads a row: thread k
-// of a row takes parts k, k + 16, ...
-__global__ __launch_bounds__(kBlock) void k_ce_rows(const float2 *part, int parts, const float *picked,
-                                                    const int32_t *target, int64_t n, float z_weight, float *loss,
-                                                    CeRow *rows)
+// Joins a row's parts, and the rows' losses. A workgroup takes kBlock / THREADS
+// rows; thread k of a row takes its parts k, k + THREADS, ... The last workgroup
+// to end adds up the sums of all of them, in their order.
+template <int THREADS>
+__global__ __launch_bounds__(kBlock) void k_ce_rows(const float2 *part, int parts, const float *picked, Targets target,
+                                                    int64_t n, float z_weight, int reduction, float *row_loss, CeRow *rows,
+                                                    LossSum *sums, int *ticket, float *loss, float *total)
 {
-    __shared__ float2 sm[16][17];
-    const int r = threadIdx.x & 15, k0 = threadIdx.x >> 4;
-    const int64_t row = (int64_t)blockIdx.x * 16 + r;
+    constexpr int ROWS = kBlock / THREADS;
+    __shared__ float2 sm[THREADS][ROWS + 1];
+    __shared__ LossSum sl[ROWS];
+    __shared__ bool is_last;
+    const int r = threadIdx.x % ROWS, k0 = threadIdx.x / ROWS;
+    const int64_t row = (int64_t)blockIdx.x * ROWS + r;
     float m = -kInf, sum = 0.0f;
-    if (row < n)
-        for (int k = k0; k < parts; k += 16) {
-            const float2 v = part[(int64_t)k * n + row];
-            const float top = fmaxf(m, v.x);
+    if (row < n) {
+        constexpr int U = 8; // loads in flight
+        for (int k = k0; k < parts; k += THREADS * U) {
+            float2 v[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int at = k + u * THREADS;
+                v[u] = at < parts ? part[(int64_t)at * n + row] : make_float2(-kInf, 0.0f);
+            }
+            float top = m;
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                top = fmaxf(top, v[u].x);
             const float base = top == -kInf ? 0.0f : top;
-            sum = sum * __expf(m - base) + v.y * __expf(v.x - base);
+            sum *= __builtin_amdgcn_exp2f(m - base);
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                sum = __builtin_fmaf(v[u].y, __builtin_amdgcn_exp2f(v[u].x - base), sum);
             m = top;
         }
+    }
     sm[k0][r] = make_float2(m, sum);
     __syncthreads();
-    if (threadIdx.x >= 16 || row >= n)
+    if constexpr (THREADS > 16) { // 16 are left, each with a fixed share
+        if (k0 < 16) {
+            float top = m;
+            for (int k = k0 + 16; k < THREADS; k += 16)
+                top = fmaxf(top, sm[k][r].x);
+            const float base = top == -kInf ? 0.0f : top;
+            sum *= __builtin_amdgcn_exp2f(m - base);
+            for (int k = k0 + 16; k < THREADS; k += 16)
+                sum = __builtin_fmaf(sm[k][r].y, __builtin_amdgcn_exp2f(sm[k][r].x - base), sum);
+            sm[k0][r] = make_float2(top, sum);
+        }
+        __syncthreads();
+    }
+    if (threadIdx.x < ROWS) {
+        LossSum mine_sum{0.0, 0};
+        if (row < n) {
+            const int t = target[row];
+            const float z = t >= 0 ? picked[row] : -kInf;
+            float top = z;
+            for (int k = 0; k < 16; ++k)
+                top = fmaxf(top, sm[k][r].x);
+            const float base = top == -kInf ? 0.0f : top;
+            double others = 0.0;
+            for (int k = 0; k < 16; ++k)
+                others += (double)sm[k][r].y * (double)exp2f(sm[k][r].x - base);
+            const double mine = t >= 0 ? (double)exp2f(z - base) : 0.0;
+            const double all = others + mine;
+            const double lse = (double)base * M_LN2 + log(all);
+            double l = mine > 0.5 ? log1p(others / mine) : lse - (double)z * M_LN2;
+            float miss = (float)(others / all);
+            if (z_weight != 0.0f)
+                l += (double)z_weight * lse * lse;
+            if (t == kIgnored)
+                l = 0.0;
+            if (t == kOutside)
+                l = miss = __builtin_nanf("");
+            mine_sum = {l, t != kIgnored};
+            if (reduction == 0)
+                row_loss[row] = (float)l;
+            if (rows)
+                rows[row] = CeRow{top, (float)(1.0 / all), miss, (float)lse};
+        }
+        sl[r] = mine_sum;
+    }
+    if (reduction == 0)
         return;
-    const int t = target[row];
-    const float z = t >= 0 ? picked[row] : -kInf;
-    float top = z;
-    for (int k = 0; k < 16; ++k)
-        top = fmaxf(top, sm[k][r].x);
-    const float base = top == -kInf ? 0.0f : top;
-    double others = 0.0;
-    for (int k = 0; k < 16; ++k)
-        others += (double)sm[k][r].y * (double)expf(sm[k][r].x - base);
-    const double mine = t >= 0 ? (double)expf(z - base) : 0.0;
-    const double total = others + mine;
-    const float lse = base + (float)log(total);
-    float l = mine > 0.5 ? (float)log1p(others / mine) : lse - z;
-    float miss = (float)(others / total);
-    l += z_weight != 0.0f ? z_weight * lse * lse : 0.0f;
-    if (t == kIgnored)
-        l = 0.0f;
-    if (t == kOutside)
-        l = miss = __builtin_nanf("");
-    loss[row] = l;
-    if (rows)
-        rows[row] = CeRow{top, (float)(1.0 / total), miss, lse};
-}
-
-// Sum (or mean over the rows that count) of the losses, in one workgroup in a
-// fixed order.
-__global__ __launch_bounds__(1024) void k_ce_total(const float *rows, const int32_t *target, int64_t n, int mean,
-                                                   float *loss, float *total)
-{
-    __shared__ double ssum[16];
-    __shared__ int scount[16];
-    double sum = 0.0;
-    int count = 0;
-    for (int64_t i = threadIdx.x; i < n; i += 1024) {
-        sum += (double)rows[i];
-        count += target[i] != kIgnored;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        LossSum s = sl[0];
+        for (int k = 1; k < ROWS; ++k) {
+            s.sum += sl[k].sum;
+            s.count += sl[k].count;
+        }
+        sums[blockIdx.x] = s;
+        __threadfence();
+        is_last = atomicAdd(ticket, 1) == (int)gridDim.x - 1;
+        __threadfence();
     }
-    sum = wave_sum(sum);
+    __syncthreads();
+    if (!is_last)
+        return;
+    __shared__ double ds[kBlock / 64];
+    __shared__ int64_t dc[kBlock / 64];
+    double a = 0.0;
+    int64_t c = 0;
+    for (unsigned i = threadIdx.x; i < gridDim.x; i += kBlock) {
+        a += sums[i].sum;
+        c += sums[i].count;
+    }
+    a = wave_sum(a);
     for (int o = 32; o > 0; o >>= 1)
-        count += __shfl_xor(count, o);
+        c += __shfl_xor(c, o);
     if (lane_id() == 0) {
-        ssum[threadIdx.x >> 6] = sum;
-        scount[threadIdx.x >> 6] = count;
+        ds[threadIdx.x >> 6] = a;
+        dc[threadIdx.x >> 6] = c;
     }
     __syncthreads();
     if (threadIdx.x == 0) {
-        for (int w = 1; w < 16; ++w) {
-            sum += ssum[w];
-            count += scount[w];
+        for (int w = 1; w < kBlock / 64; ++w) {
+            a += ds[w];
+            c += dc[w];
         }
-        loss[0] = (float)(mean ? sum / (double)max(count, 1) : sum);
+        const double counted = c > 1 ? (double)c : 1.0;
+        loss[0] = (float)(reduction == 2 ? a / counted : a);
         if (total) {
-            total[0] = (float)sum;
-            total[1] = (float)max(count, 1);
+            total[0] = (float)a;
+            total[1] = (float)counted;
         }
     }
 }
 
-// The backward pass's coefficients of a row. Its upstream gradient b and the
-// penalty's part c = 2 z_weight lse b are taken in units of a power of two at
-// least |b| + |c|, so that the stored gradient of the logits lies in [-1, 1].
-__global__ __launch_bounds__(kBlock) void k_ce_coef(const CeRow *rows, const int32_t *target, const float *grad_loss,
-                                                    const float *total, int reduction, float scale, float z_weight,
-                                                    float unit, int64_t n, CeCoef *coef, float *block_top)
-{
-    __shared__ float sm[kBlock / 64];
-    const int64_t i = (int64_t)blockIdx.x * kBlock + threadIdx.x;
-    float m = 0.0f;
-    if (i < n) {
-        const CeRow r = rows[i];
-        const int t = target[i];
-        float g = grad_loss[reduction == 0 ? i : 0];
-        if (reduction == 2)
-            g /= total[1];
-        const float b = g * scale;
-        const float c = z_weight != 0.0f ? 2.0f * z_weight * r.lse * b : 0.0f;
-        const float size = fabsf(b) + fabsf(c);
-        int e = 0;
-        if (size < kInf) // not NaN, not infinite
-            frexpf(size, &e);
-        e = min(max(e, -100), 100);
-        m = ldexpf(1.0f, e);
-        const float inv = ldexpf(1.0f, -e) * unit, mine = 1.0f - r.miss;
-        CeCoef k{r.top, (b + c) * inv * r.inv_total, (c * mine - b * r.miss) * inv, m};
-        if (t == kIgnored)
-            k.fac = k.at_target = m = 0.0f;
-        if (t == kOutside)
-            k.fac = __builtin_nanf("");
-        coef[i] = k;
+// The upstream gradient of row i, times the logits' scale.
+struct Upstream {
+    const float *grad_loss, *total;
+    int reduction;
+    float scale;
+    __device__ __forceinline__ float operator()(int64_t i) const
+    {
+        const float g = grad_loss[reduction == 0 ? i : 0];
+        return (reduction == 2 ? g / total[1] : g) * scale;
     }
-    for (int o = 32; o > 0; o >>= 1)
-        m = fmaxf(m, __shfl_xor(m, o));
+};
+
+// The largest |b| over the rows that count, of upstream gradients b, and the
+// largest |b| + |c| with the penalty's part c = 2 z_weight lse b.
+__global__ __launch_bounds__(kBlock) void k_ce_size(const CeRow *rows, Targets target, Upstream up, float z_weight,
+                                                    int64_t n, float2 *block_top)
+{
+    __shared__ float2 sm[kBlock / 64];
+    float mb = 0.0f, ms = 0.0f;
+    for (int64_t i = (int64_t)blockIdx.x * kBlock + threadIdx.x; i < n; i += (int64_t)gridDim.x * kBlock) {
+        const float b = up(i), size = fabsf(b) + (z_weight != 0.0f ? fabsf(2.0f * z_weight * rows[i].lse * b) : 0.0f);
+        if (target[i] != kIgnored && size < kInf) {
+            mb = fmaxf(mb, fabsf(b));
+            ms = fmaxf(ms, size);
+        }
+    }
+    for (int o = 32; o > 0; o >>= 1) {
+        mb = fmaxf(mb, __shfl_xor(mb, o));
+        ms = fmaxf(ms, __shfl_xor(ms, o));
+    }
     if (lane_id() == 0)
-        sm[threadIdx.x >> 6] = m;
+        sm[threadIdx.x >> 6] = make_float2(mb, ms);
     __syncthreads();
     if (threadIdx.x == 0) {
-        for (int w = 1; w < kBlock / 64; ++w)
-            m = fmaxf(m, sm[w]);
-        block_top[blockIdx.x] = m;
+        for (int w = 1; w < kBlock / 64; ++w) {
+            mb = fmaxf(mb, sm[w].x);
+            ms = fmaxf(ms, sm[w].y);
+        }
+        block_top[blockIdx.x] = make_float2(mb, ms);
     }
 }
 
-__global__ __launch_bounds__(1024) void k_ce_top(const float *block_top, int n, float *top)
+// The smallest e with size <= unit 2^e, within [-60, 20].
+__device__ __forceinline__ int exponent_over(float size, float unit)
 {
-    __shared__ float sm[16];
-    float m = 0.0f;
-    for (int i = threadIdx.x; i < n; i += 1024)
-        m = fmaxf(m, block_top[i]);
-    for (int o = 32; o > 0; o >>= 1)
-        m = fmaxf(m, __shfl_xor(m, o));
-    if (lane_id() == 0)
-        sm[threadIdx.x >> 6] = m;
-    __syncthreads();
-    if (threadIdx.x == 0) {
-        for (int w = 1; w < 16; ++w)
-            m = fmaxf(m, sm[w]);
-        *top = m > 0.0f ? m : 1.0f; // every row ignored
+    int e = 0;
+    const float f = frexpf(size / unit, &e); // in [1/2, 1)
+    if (f == 0.5f)
+        --e;
+    return size > 0.0f ? min(max(e, -60), 20) : -60;
+}
+
+// The backward pass's coefficients of a row. Its gradient is stored in units of
+// the largest upstream gradient times a power of two, so that it lies in
+// [-1, 1] and equal upstream gradients (a mean) cost the target's value -miss no
+// rounding of their own. tops: k_ce_size's, or 0 of them where all rows have the
+// same upstream gradient and no penalty.
+__global__ __launch_bounds__(kBlock) void k_ce_coef(const CeRow *rows, Targets target, Upstream up, float z_weight,
+                                                    float stored_unit, int64_t n, const float2 *block_top, int tops,
+                                                    CeCoef *coef, CeTop *top)
+{
+    __shared__ float2 sm[kBlock / 64];
+    float mb = 0.0f, ms = 0.0f;
+    for (int i = threadIdx.x; i < tops; i += kBlock) {
+        mb = fmaxf(mb, block_top[i].x);
+        ms = fmaxf(ms, block_top[i].y);
     }
+    for (int o = 32; o > 0; o >>= 1) {
+        mb = fmaxf(mb, __shfl_xor(mb, o));
+        ms = fmaxf(ms, __shfl_xor(ms, o));
+    }
+    if (lane_id() == 0)
+        sm[threadIdx.x >> 6] = make_float2(mb, ms);
+    __syncthreads();
+    for (int w = 0; w < kBlock / 64; ++w) {
+        mb = fmaxf(mb, sm[w].x);
+        ms = fmaxf(ms, sm[w].y);
+    }
+    if (tops == 0)
+        mb = ms = fabsf(up(0));
+    // within 2^+-60: its smallest and largest multiples stay normal
+    const float unit = mb >= 0x1p-60f && mb <= 0x1p60f ? mb : 1.0f;
+    const float largest = ldexpf(unit, max(exponent_over(ms, unit), 0));
+    if (blockIdx.x == 0 && threadIdx.x == 0)
+        *top = CeTop{unit, largest};
+    const int64_t i = (int64_t)blockIdx.x * kBlock + threadIdx.x;
+    if (i >= n)
+        return;
+    const CeRow r = rows[i];
+    const int t = target[i];
+    const float b = up(i), c = z_weight != 0.0f ? 2.0f * z_weight * r.lse * b : 0.0f;
+    const float size = fabsf(b) + fabsf(c);
+    const float mine = ldexpf(unit, size < kInf ? exponent_over(size, unit) : 0);
+    const float bn = b / mine * stored_unit, cn = c / mine * stored_unit;
+    CeCoef k{r.top, (bn + cn) * r.inv_total, cn * (1.0f - r.miss) - bn * r.miss, mine};
+    if (t == kIgnored)
+        k = CeCoef{0.0f, 0.0f, 0.0f, unit};
+    if (t == kOutside)
+        k.fac = __builtin_nanf("");
+    coef[i] = k;
 }
 
 // Adds up the parts of a gradient and rounds it.
 template <class OUT>
 __global__ __launch_bounds__(kBlock) void k_ce_join(const float *part, int splits, int64_t split, int cols, int ld,
-                                                    int64_t rows, const CeCoef *coef, const float *top, float inv_unit,
+                                                    int64_t rows, const CeCoef *coef, const CeTop *top, float inv_unit,
                                                     void *out)
 {
     const int64_t i = ((int64_t)blockIdx.x * kBlock + threadIdx.x) * 4;
@@ -720,7 +934,7 @@ __global__ __launch_bounds__(kBlock) void k_ce_join(const float *part, int split
     f32x4 v = *(const f32x4 *)(part + i);
     for (int s = 1; s < splits; ++s)
         v += *(const f32x4 *)(part + s * split + i);
-    v *= (coef ? coef[r].unit : *top) * inv_unit;
+    v *= (coef ? coef[r].unit : top->top) * inv_unit;
 #pragma unroll
     for (int u = 0; u < 4; ++u)
         if (c + u < cols)
@@ -798,14 +1012,39 @@ void choose_packs(const CeProblem &p, bool *x, bool *w)
     *w = p.type == ElemType::f32 || p.dim % 8 || !aligned16(p.w);
 }
 
-template <class IN>
-void launch_pack(const void *in, uint16_t *out, int64_t samples, int rows, int rows_out, int dim, int dim_pad,
-                 const CeCoef *coef, const float *top, hipStream_t s)
+// The copies that a pass needs, in one launch.
+struct Packs {
+    PackJobs jobs{};
+    int n = 0;
+    unsigned blocks = 0;
+    void add(const void *in, uint16_t *out, int64_t samples, int rows, int rows_out, const CeCoef *coef)
+    {
+        PackJob &j = jobs.job[n++];
+        j.in = in;
+        j.out = out;
+        j.n = samples * rows_out * jobs.dim_pad;
+        j.rows = rows;
+        j.rows_out = rows_out;
+        j.coef = coef;
+        j.blocks = blocks_for(j.n / 8, kBlock);
+        blocks += j.blocks;
+    }
+    template <class IN> void launch(hipStream_t s) const
+    {
+        if (n)
+            k_ce_pack<IN><<<dim3(blocks), dim3(kBlock), 0, s>>>(jobs);
+    }
+};
+
+// The logits' scale in units of log 2; never 0, by which a class that is not
+// there (an infinite logit) would become NaN.
+float scale2_of(const CeProblem &p)
 {
-    const int64_t n = samples * rows_out * dim_pad;
-    k_ce_pack<IN><<<dim3(blocks_for(n / 4, kBlock)), dim3(kBlock), 0, s>>>(in, out, n, rows, rows_out, dim, dim_pad, n,
-                                                                          coef, top);
+    const float s = p.scale * kLog2E;
+    return std::abs(s) < FLT_MIN ? std::copysign(FLT_MIN, s) : s;
 }
+
+Targets targets_of(const CeProblem &p) { return {p.target, p.target32, p.classes, p.ignore_index}; }
 
 // x, w as operands with the features contiguous.
 Operand features(const CeProblem &p, bool packed, const void *user, const uint16_t *copy, int64_t rows, int dim_pad)
@@ -832,6 +1071,11 @@ template <class F> void by_type(ElemType t, F f)
 
 } // namespace
 
+// Threads of k_ce_rows a row: with few rows, as many as it takes to have the
+// parts' loads in flight together (one row of 131072 classes, 4096 parts: 16
+// threads 105 us).
+static int row_threads(int64_t n) { return n >= 4096 ? 16 : kBlock; }
+
 CeForwardPlan ce_plan_forward(const CeProblem &p)
 {
     CeForwardPlan f{};
@@ -843,9 +1087,10 @@ CeForwardPlan ce_plan_forward(const CeProblem &p)
     Offsets o;
     f.x = o.take(f.pack_x ? n * f.dim_pad * 2 * planes(p) : 0);
     f.w = o.take(f.pack_w ? (int64_t)p.samples * p.classes * f.dim_pad * 2 * planes(p) : 0);
-    f.target = o.take(n * sizeof(int32_t));
     f.part = o.take((int64_t)f.parts * n * sizeof(float2));
-    f.picked = o.take(2 * n * sizeof(float));
+    f.picked = o.take(n * sizeof(float));
+    f.sums = o.take(p.reduction == 0 ? 0 : blocks_for(n, kBlock / row_threads(n)) * sizeof(LossSum));
+    f.ticket = o.take(sizeof(int));
     f.bytes = o.at;
     return f;
 }
@@ -854,20 +1099,23 @@ void ce_forward(const CeProblem &p, const CeForwardPlan &plan, uint8_t *ws, floa
                 hipStream_t s)
 {
     const int64_t n = all_rows(p);
-    auto *target = (int32_t *)(ws + plan.target);
     auto *part = (float2 *)(ws + plan.part);
     auto *picked = (float *)(ws + plan.picked);
-    float *row_loss = p.reduction == 0 ? loss : picked + n;
-    k_ce_targets<<<dim3(blocks_for(n, kBlock)), dim3(kBlock), 0, s>>>(p.target, p.target32, p.ignore_index, p.classes,
-                                                                     target, n);
+    auto *sums = (LossSum *)(ws + plan.sums);
+    auto *ticket = (int *)(ws + plan.ticket);
+    const Targets target = targets_of(p);
     auto *x = (uint16_t *)(ws + plan.x), *w = (uint16_t *)(ws + plan.w);
     by_type(p.type, [&](auto elem, auto cut, auto io) {
         using ELEM = decltype(elem);
         using IO = decltype(io);
+        Packs packs;
+        packs.jobs.dim = p.dim;
+        packs.jobs.dim_pad = plan.dim_pad;
         if (plan.pack_x)
-            launch_pack<IO>(p.x, x, p.samples, p.rows, p.rows, p.dim, plan.dim_pad, nullptr, nullptr, s);
+            packs.add(p.x, x, p.samples, p.rows, p.rows, nullptr);
         if (plan.pack_w)
-            launch_pack<IO>(p.w, w, p.samples, p.classes, p.classes, p.dim, plan.dim_pad, nullptr, nullptr, s);
+            packs.add(p.w, w, p.samples, p.classes, p.classes, nullptr);
+        packs.launch<IO>(s);
         Product a{};
         a.p = features(p, plan.pack_w, p.w, w, p.classes, plan.dim_pad);
         a.q = features(p, plan.pack_x, p.x, x, p.rows, plan.dim_pad);
@@ -876,12 +1124,14 @@ void ce_forward(const CeProblem &p, const CeForwardPlan &plan, uint8_t *ws, floa
         a.splits = 1;
         launch_product<ELEM, decltype(cut)::value, false, false>(choose(p.classes, p.rows, p.samples, true), a,
                                                                  p.classes, p.rows,
-                                                                 FinishStats{target, part, picked, p.scale}, s);
+                                                                 FinishStats{target, part, picked, ticket, scale2_of(p)}, s);
     });
-    k_ce_rows<<<dim3(blocks_for(n, 16)), dim3(kBlock), 0, s>>>(part, plan.parts, picked, target, n, p.z_weight, row_loss,
-                                                              rows);
-    if (p.reduction != 0)
-        k_ce_total<<<dim3(1), dim3(1024), 0, s>>>(row_loss, target, n, p.reduction == 2, loss, total);
+    if (row_threads(n) == 16)
+        k_ce_rows<16><<<dim3(blocks_for(n, kBlock / 16)), dim3(kBlock), 0, s>>>(
+            part, plan.parts, picked, target, n, p.z_weight, p.reduction, loss, rows, sums, ticket, loss, total);
+    else
+        k_ce_rows<kBlock><<<dim3(blocks_for(n, 1)), dim3(kBlock), 0, s>>>(
+            part, plan.parts, picked, target, n, p.z_weight, p.reduction, loss, rows, sums, ticket, loss, total);
 }
 
 namespace {
@@ -929,10 +1179,10 @@ CeBackwardPlan ce_plan_backward(const CeProblem &p, bool want_x, bool want_w)
     Offsets o;
     b.x = o.take(b.pack_x ? n * b.dim_pad * size : 0);
     b.w = o.take(b.pack_w ? (int64_t)p.samples * p.classes * b.dim_pad * size : 0);
-    b.target = o.take(n * sizeof(int32_t));
     b.coef = o.take(n * sizeof(CeCoef));
-    b.block_top = o.take(blocks_for(n, kBlock) * sizeof(float));
-    b.top = o.take(sizeof(float));
+    b.tops = p.reduction == 0 || p.z_weight != 0.0f ? (int)std::min<int64_t>(512, blocks_for(n, kBlock)) : 0;
+    b.block_top = o.take(b.tops * sizeof(float2));
+    b.top = o.take(sizeof(CeTop));
     b.xs = o.take(want_w ? (int64_t)p.samples * b.rows_pad * b.dim_pad * size : 0);
     b.g = o.take((int64_t)b.piece_samples * b.rows_pad * b.ld_g * size);
     b.part_x = o.take(want_x && b.sum_x ? (int64_t)b.split_x * b.piece_samples * p.rows * ld * 4 : 0);
@@ -945,30 +1195,35 @@ void ce_backward(const CeProblem &p, const CeBackwardPlan &plan, uint8_t *ws, co
                  const float *grad_loss, void *grad_x, void *grad_w, hipStream_t s)
 {
     const int64_t n = all_rows(p);
-    auto *target = (int32_t *)(ws + plan.target);
     auto *coef = (CeCoef *)(ws + plan.coef);
-    auto *block_top = (float *)(ws + plan.block_top), *top = (float *)(ws + plan.top);
+    auto *block_top = (float2 *)(ws + plan.block_top);
+    auto *top = (CeTop *)(ws + plan.top);
+    const Targets target = targets_of(p);
+    const Upstream up{grad_loss, total, p.reduction, p.scale};
     auto *x = (uint16_t *)(ws + plan.x), *w = (uint16_t *)(ws + plan.w);
     auto *xs = (uint16_t *)(ws + plan.xs), *g = (uint16_t *)(ws + plan.g);
     auto *part_x = (float *)(ws + plan.part_x), *part_w = (float *)(ws + plan.part_w);
     const int64_t ld = pad_to(p.dim, 4);
-    k_ce_targets<<<dim3(blocks_for(n, kBlock)), dim3(kBlock), 0, s>>>(p.target, p.target32, p.ignore_index, p.classes,
-                                                                     target, n);
     by_type(p.type, [&](auto elem, auto cut, auto io) {
         using ELEM = decltype(elem);
         using IO = decltype(io);
         constexpr bool PLANES = decltype(cut)::value;
         const float inv_unit = 1.0f / ELEM::kUnit;
-        const unsigned blocks = blocks_for(n, kBlock);
-        k_ce_coef<<<dim3(blocks), dim3(kBlock), 0, s>>>(rows, target, grad_loss, total, p.reduction, p.scale, p.z_weight,
-                                                        ELEM::kUnit, n, coef, block_top);
-        k_ce_top<<<dim3(1), dim3(1024), 0, s>>>(block_top, (int)blocks, top);
+        if (plan.tops)
+            k_ce_size<<<dim3(plan.tops), dim3(kBlock), 0, s>>>(rows, target, up, p.z_weight, n, block_top);
+        k_ce_coef<<<dim3(blocks_for(n, kBlock)), dim3(kBlock), 0, s>>>(rows, target, up, p.z_weight, ELEM::kUnit, n,
+                                                                      block_top, plan.tops, coef, top);
+        Packs packs;
+        packs.jobs.dim = p.dim;
+        packs.jobs.dim_pad = plan.dim_pad;
+        packs.jobs.top = top;
         if (plan.pack_x)
-            launch_pack<IO>(p.x, x, p.samples, p.rows, p.rows, p.dim, plan.dim_pad, nullptr, nullptr, s);
+            packs.add(p.x, x, p.samples, p.rows, p.rows, nullptr);
         if (plan.pack_w)
-            launch_pack<IO>(p.w, w, p.samples, p.classes, p.classes, p.dim, plan.dim_pad, nullptr, nullptr, s);
+            packs.add(p.w, w, p.samples, p.classes, p.classes, nullptr);
         if (grad_w)
-            launch_pack<IO>(p.x, xs, p.samples, p.rows, plan.rows_pad, p.dim, plan.dim_pad, coef, top, s);
+            packs.add(p.x, xs, p.samples, p.rows, plan.rows_pad, coef);
+        packs.launch<IO>(s);
         const Operand W = features(p, plan.pack_w, p.w, w, p.classes, plan.dim_pad);
         const Operand X = features(p, plan.pack_x, p.x, x, p.rows, plan.dim_pad);
         for (int s0 = 0; s0 < p.samples; s0 += plan.piece_samples) {
@@ -990,7 +1245,7 @@ void ce_backward(const CeProblem &p, const CeBackwardPlan &plan, uint8_t *ws, co
                     const int64_t r0 = (int64_t)s0 * p.rows;
                     launch_product<ELEM, PLANES, false, false>(
                         choose(nc, p.rows, ns, true), a, nc_pad, plan.rows_pad,
-                        FinishGrad<PLANES>{target + r0, coef + r0, g, plane_g, p.scale, plan.rows_pad, plan.ld_g, c0}, s);
+                        FinishGrad<PLANES>{target, coef, r0, g, plane_g, scale2_of(p), plan.rows_pad, plan.ld_g, c0}, s);
                 }
                 Operand G;
                 G.base = g;

@@ -57,6 +57,9 @@ def linear_ce(x, w, target, *, scale=1.0, z_weight=0.0, ignore_index=-100, reduc
         rel = (4 * tz + 2 * EXP).unsqueeze(1) + u + 2.0 ** -20
         floor = m * 2.0 ** -39 if dtype == torch.float16 else m * 2.0 ** -120
         dG = A * rel + torch.where(used[s].unsqueeze(1), floor, 0.0)
+        # scale, g / n and their product are float32: below 2^-126 each is off by up
+        # to 2^-150, half a step of the subnormal numbers, whatever its size
+        dG = dG + 2.0 ** -150 * (2 + up[s].abs().unsqueeze(1) + abs(scale)) * torch.where(used[s].unsqueeze(1), 1.0, 0.0)
         gx, gw = G @ ws, G.T @ xs
         out["gx"].append(gx)
         out["gx_tol"].append(dG @ ws.abs() + A @ ws.abs() * (V + 64) * 2.0 ** -24 + u * gx.abs() + SMALLEST[dtype])

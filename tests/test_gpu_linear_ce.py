@@ -155,6 +155,24 @@ def test_logits_beyond_the_exponentials_range():
     check(x, w, t, reduction="none", scale=-3000.0)
 
 
+@pytest.mark.parametrize("scale", [0.0, -0.0, 1e-40])
+def test_scales_of_nothing(scale):
+    x, w, t = make(0, 40, 61, 64, F32, ignored=0.2)
+    loss, gx, gw = check(x, w, t, reduction="none", scale=scale)
+    assert (gx.abs() <= 1e-30).all() and (gw.abs() <= 1e-30).all()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16, F16], ids=["f32", "bf16", "f16"])
+@pytest.mark.parametrize("size", [1e-30, 1e-12, 1e6, 1e30])
+def test_upstream_gradients_of_any_size(dtype, size):
+    if dtype == F16 and size == 1e30:
+        pytest.skip("every gradient is beyond half precision")
+    x, w, t = make(0, 40, 61, 64, dtype)
+    for reduction in ("none", "sum"):
+        check(x, w, t, reduction=reduction, z_weight=0.3, grad_loss=torch.full(t.shape if reduction == "none" else (), size,
+                                                                              device="cuda"))
+
+
 def test_rows_and_classes_that_are_equal():
     x, w, t = make(0, 40, 300, 64, BF16)
     w[:] = w[0]
