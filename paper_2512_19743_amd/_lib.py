@@ -416,15 +416,22 @@ class _Queued:
     def __init__(self, device: torch.device, stream: Optional[torch.cuda.Stream]):
         if stream is not None and stream.device != device:
             raise ValueError(f"stream must be on {device}, got {stream.device}")
-        self.guard = torch.cuda.stream(stream) if stream is not None else torch.cuda.device(device)
+        self.guard = None
+        if stream is not None:
+            self.guard = torch.cuda.stream(stream)
+        elif torch.cuda.current_device() != device.index:
+            self.guard = torch.cuda.device(device)
         self.device, self.stream = device, stream
 
     def __enter__(self):
-        self.guard.__enter__()
+        if self.guard is not None:
+            self.guard.__enter__()
         return _stream_handle(self.stream, self.device)
 
     def __exit__(self, *exc):
-        return self.guard.__exit__(*exc)
+        if self.guard is not None:
+            self.guard.__exit__(*exc)
+        return False
 
 
 def _linear_ce_desc(x, w, target, scale, z_weight, ignore_index, reduction) -> apml_linear_ce_desc:

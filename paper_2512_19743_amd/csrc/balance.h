@@ -26,7 +26,7 @@ struct BalanceProblem {
 
 struct BalancePlan {
     int chunks, tokens; // chunks of tokens a sample, tokens of a chunk
-    size_t p, count, z, n, loss, bytes;
+    size_t p, count, z, loss, ticket, bytes;
 };
 BalancePlan balance_plan(const BalanceProblem &p);
 // state: [samples][experts + 1] floats (E f_e, then 1 / valid tokens), or NULL.

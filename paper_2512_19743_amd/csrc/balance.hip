@@ -44,17 +44,34 @@ template <class T, int VEC> struct alignas(sizeof(T) * VEC) Pack {
     T v[VEC];
 };
 
+// Butterfly over an aligned group of lanes, all of which end with the same bits.
+template <class F> __device__ __forceinline__ float group_reduce(float v, int lanes, F f)
+{
+    const auto step = [&](auto k) {
+        constexpr int K = decltype(k)::value;
+        v = f(v, __builtin_bit_cast(float, partner<K>(__builtin_bit_cast(int, v))));
+    };
+    if (lanes > 1)
+        step(std::integral_constant<int, 0>{});
+    if (lanes > 2)
+        step(std::integral_constant<int, 1>{});
+    if (lanes > 4)
+        step(std::integral_constant<int, 2>{});
+    if (lanes > 8)
+        step(std::integral_constant<int, 3>{});
+    if (lanes > 16)
+        step(std::integral_constant<int, 4>{});
+    if (lanes > 32)
+        step(std::integral_constant<int, 5>{});
+    return v;
+}
 __device__ __forceinline__ float group_max(float v, int lanes)
 {
-    for (int o = 1; o < lanes; o <<= 1)
-        v = fmaxf(v, __shfl_xor(v, o));
-    return v;
+    return group_reduce(v, lanes, [](float a, float b) { return fmaxf(a, b); });
 }
 __device__ __forceinline__ float group_add(float v, int lanes)
 {
-    for (int o = 1; o < lanes; o <<= 1)
-        v += __shfl_xor(v, o);
-    return v;
+    return group_reduce(v, lanes, [](float a, float b) { return a + b; });
 }
 
 // Columns of a lane: VEC neighbours at (i * lanes + lane) * VEC, i < NV.
@@ -76,6 +93,44 @@ __device__ __forceinline__ void load_row(const typename L::raw *row, int lane, i
                 v[i * VEC + u] = -kInf;
         }
     }
+}
+
+// Rows that cannot be read 16 bytes at a time pass through shared memory: their
+// tokens lie one after another, so a tile of them is read in whole 16-byte words
+// wherever it starts (161 experts in half precision: element by element 1.4 TB/s).
+// An element keeps its place within its word; returns the first one's.
+template <class R> __device__ __forceinline__ R *tile_in(R *lds, const R *src, int n)
+{
+    constexpr int W = 16 / sizeof(R);
+    const int shift = (int)(((uintptr_t)src & 15) / sizeof(R));
+    const int head = min(n, (W - shift) % W), words = (n - head) / W;
+    R *to = lds + shift;
+    for (int i = threadIdx.x; i < words; i += kBlock)
+        *(Pack<R, W> *)(to + head + i * W) = *(const Pack<R, W> *)(src + head + i * W);
+    const int tail = head + words * W;
+    if ((int)threadIdx.x < head)
+        to[threadIdx.x] = src[threadIdx.x];
+    if ((int)threadIdx.x < n - tail)
+        to[tail + threadIdx.x] = src[tail + threadIdx.x];
+    return to;
+}
+template <class R> __device__ __forceinline__ void tile_out(R *dst, const R *from, int n)
+{
+    constexpr int W = 16 / sizeof(R);
+    if ((((uintptr_t)dst ^ (uintptr_t)(__attribute__((address_space(3))) const R *)from) & 15) != 0) {
+        for (int i = threadIdx.x; i < n; i += kBlock)
+            dst[i] = from[i];
+        return;
+    }
+    const int shift = (int)(((uintptr_t)dst & 15) / sizeof(R));
+    const int head = min(n, (W - shift) % W), words = (n - head) / W;
+    for (int i = threadIdx.x; i < words; i += kBlock)
+        *(Pack<R, W> *)(dst + head + i * W) = *(const Pack<R, W> *)(from + head + i * W);
+    const int tail = head + words * W;
+    if ((int)threadIdx.x < head)
+        dst[threadIdx.x] = from[threadIdx.x];
+    if ((int)threadIdx.x < n - tail)
+        dst[tail + threadIdx.x] = from[tail + threadIdx.x];
 }
 
 // v becomes exp(v - max); returns the log-sum-exp, and 1 / sum in *inv (0 for a
@@ -126,22 +181,26 @@ struct BalanceArgs {
     const void *logits, *index;
     const uint8_t *valid;
     int tokens, E, chosen, chunk, chunks, lanes;
+    int tile;      // tokens that pass through shared memory at a time
     float z_weight;
     float *p;      // [samples][chunks][E]
     int32_t *count;
     ChunkSum *z;   // [samples][chunks]
+    int *ticket;   // cleared for k_balance_join
 };
 
 template <class L, int VEC, int NV>
 __global__ __launch_bounds__(kBlock) void k_balance_chunks(BalanceArgs a, bool index32)
 {
-    extern __shared__ float sm[]; // [E] sums, then [E] counts
+    extern __shared__ __attribute__((aligned(16))) float sm[]; // [E] sums, then [E] counts
     __shared__ float sz[kBlock / 64];
     __shared__ int sn[kBlock / 64];
     int *hist = (int *)(sm + a.E);
     const int sample = blockIdx.x / a.chunks, chunk = blockIdx.x % a.chunks;
     const int t0 = chunk * a.chunk, t1 = min(t0 + a.chunk, a.tokens);
     const int lane = threadIdx.x & (a.lanes - 1), group = threadIdx.x / a.lanes, groups = kBlock / a.lanes;
+    if (blockIdx.x == 0 && threadIdx.x == 0)
+        *a.ticket = 0;
     for (int e = threadIdx.x; e < a.E; e += kBlock) {
         sm[e] = 0.0f;
         hist[e] = 0;
@@ -160,18 +219,44 @@ __global__ __launch_bounds__(kBlock) void k_balance_chunks(BalanceArgs a, bool i
         acc[i] = 0.0f;
     float z = 0.0f;
     int n = 0;
-    for (int t = t0 + group; t < t1; t += groups) {
-        const int64_t r = row0 + t;
-        if (a.valid && !a.valid[r])
-            continue;
-        float v[NV * VEC], inv;
-        load_row<L, VEC, NV>((const typename L::raw *)a.logits + r * a.E, lane, a.lanes, a.E, v);
+    const auto add = [&](float (&v)[NV * VEC]) {
+        float inv;
         const float lse = exp_row(v, a.lanes, &inv);
 #pragma unroll
         for (int i = 0; i < NV * VEC; ++i)
             acc[i] = __builtin_fmaf(v[i], inv, acc[i]);
         z = __builtin_fmaf(lse, lse, z);
         ++n;
+    };
+    if constexpr (VEC > 1) {
+        for (int t = t0 + group; t < t1; t += 2 * groups) { // two rows' loads in flight
+            const int64_t r = row0 + t, q = r + groups;
+            const bool two = t + groups < t1;
+            const bool vr = !a.valid || a.valid[r], vq = two && (!a.valid || a.valid[q]);
+            float v[NV * VEC], w[NV * VEC];
+            load_row<L, VEC, NV>((const typename L::raw *)a.logits + r * a.E, lane, a.lanes, a.E, v);
+            load_row<L, VEC, NV>((const typename L::raw *)a.logits + (two ? q : r) * a.E, lane, a.lanes, a.E, w);
+            if (vr)
+                add(v);
+            if (vq)
+                add(w);
+        }
+    } else {
+        using R = typename L::raw;
+        R *lds = (R *)(sm + ((2 * a.E + 3) & ~3));
+        for (int b = t0; b < t1; b += a.tile) {
+            const int n_tok = min(a.tile, t1 - b);
+            __syncthreads();
+            const R *rows = tile_in(lds, (const R *)a.logits + (row0 + b) * a.E, n_tok * a.E);
+            __syncthreads();
+            for (int t = group; t < n_tok; t += groups) {
+                if (a.valid && !a.valid[row0 + b + t])
+                    continue;
+                float v[NV * VEC];
+                load_row<L, VEC, NV>(rows + t * a.E, lane, a.lanes, a.E, v);
+                add(v);
+            }
+        }
     }
     // the groups of a wave, then the waves one after another: a fixed order
     for (int o = a.lanes; o < 64; o <<= 1) {
@@ -215,13 +300,21 @@ __global__ __launch_bounds__(kBlock) void k_balance_chunks(BalanceArgs a, bool i
     }
 }
 
+// A chunk's share of an expert.
+struct Share {
+    float p;
+    int count;
+};
+
 // Joins a sample's chunks: one workgroup a sample.
-__global__ __launch_bounds__(1024) void k_balance_join(BalanceArgs a, int64_t *counts, float *loss, float *state)
+__global__ __launch_bounds__(1024) void k_balance_join(BalanceArgs a, int64_t *counts, float *loss, float *state,
+                                                       int reduction, float *per, int *ticket)
 {
     __shared__ double ssum[3][16]; // per wave
     __shared__ double total[3];
     __shared__ double sp[1024];
     __shared__ long long sc[1024];
+    __shared__ bool is_last;
     const int sample = blockIdx.x;
     const int64_t base = (int64_t)sample * a.chunks;
     // 1024 / width threads an expert, each with every so-manieth chunk
@@ -232,11 +325,15 @@ __global__ __launch_bounds__(1024) void k_balance_join(BalanceArgs a, int64_t *c
     double p = 0.0;
     long long c = 0;
     if (e < a.E)
-        for (int k = k0; k < a.chunks; k += step) {
-            p += (double)a.p[(base + k) * a.E + e];
-            if (a.index)
-                c += a.count[(base + k) * a.E + e];
-        }
+        strided<8>(
+            k0, a.chunks, step,
+            [&](int k) {
+                return Share{a.p[(base + k) * a.E + e], a.index ? a.count[(base + k) * a.E + e] : 0};
+            },
+            [&](Share v, int) {
+                p += (double)v.p;
+                c += v.count;
+            });
     sp[threadIdx.x] = p;
     sc[threadIdx.x] = c;
     double z = 0.0, n = 0.0;
@@ -290,20 +387,29 @@ __global__ __launch_bounds__(1024) void k_balance_join(BalanceArgs a, int64_t *c
         v *= inv_n;
         if (a.z_weight != 0.0f)
             v += (double)a.z_weight * zz * inv_n;
-        loss[sample] = (float)v;
         if (state)
             state[(int64_t)sample * (a.E + 1) + a.E] = (float)inv_n;
+        if (reduction == 0 || gridDim.x == 1) {
+            loss[sample] = (float)v;
+        } else {
+            // device-scope accesses go past the XCDs' own L2s: the wait is all
+            // the order that the ticket needs
+            __hip_atomic_store(&per[sample], (float)v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            is_last = __hip_atomic_fetch_add(ticket, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (int)gridDim.x - 1;
+        }
     }
-}
-
-__global__ __launch_bounds__(64) void k_balance_total(const float *per, int n, int mean, float *loss)
-{
-    double v = 0.0;
-    for (int i = threadIdx.x; i < n; i += 64)
-        v += (double)per[i];
+    if (reduction == 0 || gridDim.x == 1)
+        return;
+    __syncthreads();
+    if (!is_last || threadIdx.x >= 64)
+        return;
+    double v = 0.0; // the samples in their order, by the last workgroup to end
+    for (int i = threadIdx.x; i < (int)gridDim.x; i += 64)
+        v += (double)__hip_atomic_load(&per[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     v = wave_sum(v);
     if (threadIdx.x == 0)
-        loss[0] = (float)(mean ? v / n : v);
+        loss[0] = (float)(reduction == 2 ? v / (double)gridDim.x : v);
 }
 
 template <class L, int VEC, int NV>
@@ -324,13 +430,9 @@ __global__ __launch_bounds__(kBlock) void k_balance_grad(BalanceArgs a, const fl
             f[i * VEC + u] = c < a.E ? load[c] : 0.0f;
         }
     const int64_t row0 = (int64_t)sample * a.tokens;
-    for (int t = t0 + group; t < t1; t += groups) {
-        const int64_t r = row0 + t;
-        const bool valid = !a.valid || a.valid[r];
-        float v[NV * VEC];
+    const auto finish = [&](float (&v)[NV * VEC], bool valid, typename L::raw *to) {
         if (valid) {
             float inv, dot = 0.0f;
-            load_row<L, VEC, NV>((const typename L::raw *)a.logits + r * a.E, lane, a.lanes, a.E, v);
             const float lse = exp_row(v, a.lanes, &inv);
 #pragma unroll
             for (int i = 0; i < NV * VEC; ++i)
@@ -349,8 +451,38 @@ __global__ __launch_bounds__(kBlock) void k_balance_grad(BalanceArgs a, const fl
 #pragma unroll
                 for (int u = 0; u < VEC; ++u)
                     p.v[u] = L::from(valid ? v[i * VEC + u] : 0.0f);
-                *(Pack<typename L::raw, VEC> *)((typename L::raw *)out + r * a.E + c) = p;
+                *(Pack<typename L::raw, VEC> *)(to + c) = p;
             }
+        }
+    };
+    if constexpr (VEC > 1) {
+        for (int t = t0 + group; t < t1; t += 2 * groups) { // two rows' loads in flight
+            const int64_t r = row0 + t, q = r + groups;
+            const bool two = t + groups < t1;
+            const bool vr = !a.valid || a.valid[r], vq = two && (!a.valid || a.valid[q]);
+            float v[NV * VEC], w[NV * VEC];
+            load_row<L, VEC, NV>((const typename L::raw *)a.logits + r * a.E, lane, a.lanes, a.E, v);
+            load_row<L, VEC, NV>((const typename L::raw *)a.logits + (two ? q : r) * a.E, lane, a.lanes, a.E, w);
+            finish(v, vr, (typename L::raw *)out + r * a.E);
+            if (two)
+                finish(w, vq, (typename L::raw *)out + q * a.E);
+        }    } else {
+        extern __shared__ __attribute__((aligned(16))) float sm[];
+        using R = typename L::raw;
+        R *lds = (R *)sm;
+        for (int b = t0; b < t1; b += a.tile) {
+            const int n_tok = min(a.tile, t1 - b);
+            const int64_t at = (row0 + b) * a.E;
+            __syncthreads();
+            R *rows = tile_in(lds, (const R *)a.logits + at, n_tok * a.E);
+            __syncthreads();
+            for (int t = group; t < n_tok; t += groups) {
+                float v[NV * VEC];
+                load_row<L, VEC, NV>(rows + t * a.E, lane, a.lanes, a.E, v);
+                finish(v, !a.valid || a.valid[row0 + b + t], rows + t * a.E);
+            }
+            __syncthreads();
+            tile_out((R *)out + at, rows, n_tok * a.E);
         }
     }
 }
@@ -393,10 +525,11 @@ RowShape row_shape(const BalanceProblem &p, const void *grad)
     RowShape r{1, 1, 1};
     if (p.experts % wide == 0 && ((uintptr_t)p.logits & 15) == 0 && ((uintptr_t)grad & 15) == 0)
         r.vec = wide;
+    // 16 lanes, whose exchanges need no shared memory, take up to 4 packs each
+    // (16 single columns); more lanes what is left
     const int packs = (p.experts + r.vec - 1) / r.vec;
-    r.nv = packs >= 4 ? 4 : 1;
-    if (r.vec == 1 && packs > 256)
-        r.nv = 16;
+    const int most = r.vec > 1 ? 4 : 16;
+    r.nv = packs <= 16 ? 1 : packs <= 64 || r.vec > 1 ? 4 : most;
     while (r.lanes * r.nv < packs)
         r.lanes <<= 1;
     return r;
@@ -434,6 +567,18 @@ void cut_tokens(const BalanceProblem &p, int64_t blocks, int least, int *chunk, 
     *chunks = (p.tokens + *chunk - 1) / *chunk;
 }
 
+// Tokens that pass through shared memory at a time: 16 KB of them, at least one a
+// lane group.
+int tile_tokens(const BalanceProblem &p, const RowShape &r)
+{
+    const int groups = kBlock / r.lanes, row = p.experts * (int)elem_size(p.type);
+    return groups * std::max(1, 16384 / (row * groups));
+}
+size_t tile_bytes(const BalanceProblem &p, const RowShape &r)
+{
+    return r.vec > 1 ? 0 : (size_t)tile_tokens(p, r) * p.experts * elem_size(p.type) + 32;
+}
+
 // A few tokens a lane group of a workgroup, whose size grows with the experts.
 int least_tokens(const BalanceProblem &p) { return std::min(512, std::max(16, 8192 / p.experts)); }
 
@@ -455,7 +600,7 @@ BalanceArgs args_of(const BalanceProblem &p)
 BalancePlan balance_plan(const BalanceProblem &p)
 {
     BalancePlan b{};
-    cut_tokens(p, 2048, least_tokens(p), &b.tokens, &b.chunks);
+    cut_tokens(p, 1024, least_tokens(p), &b.tokens, &b.chunks);
     size_t at = 0;
     const auto take = [&](size_t bytes) {
         const size_t o = at;
@@ -467,6 +612,7 @@ BalancePlan balance_plan(const BalanceProblem &p)
     b.count = take(parts * p.experts * sizeof(int32_t));
     b.z = take(parts * sizeof(ChunkSum));
     b.loss = take(p.samples * sizeof(float));
+    b.ticket = take(sizeof(int));
     b.bytes = at;
     return b;
 }
@@ -479,17 +625,18 @@ void balance_forward(const BalanceProblem &p, const BalancePlan &plan, uint8_t *
     a.chunk = plan.tokens;
     a.chunks = plan.chunks;
     a.lanes = r.lanes;
+    a.tile = tile_tokens(p, r);
     a.p = (float *)(ws + plan.p);
     a.count = (int32_t *)(ws + plan.count);
     a.z = (ChunkSum *)(ws + plan.z);
-    float *per = p.reduction == 0 || p.samples == 1 ? loss : (float *)(ws + plan.loss);
+    a.ticket = (int *)(ws + plan.ticket);
     by_shape(p.type, r, [&](auto l, auto vec, auto nv) {
         k_balance_chunks<decltype(l), decltype(vec)::value, decltype(nv)::value>
-            <<<dim3((unsigned)(p.samples * a.chunks)), dim3(kBlock), 2 * p.experts * sizeof(float), s>>>(a, p.index32);
+            <<<dim3((unsigned)(p.samples * a.chunks)), dim3(kBlock),
+               ((2 * p.experts + 3) & ~3) * sizeof(float) + tile_bytes(p, r), s>>>(a, p.index32);
     });
-    k_balance_join<<<dim3(p.samples), dim3(1024), 0, s>>>(a, counts, per, state);
-    if (per != loss)
-        k_balance_total<<<dim3(1), dim3(64), 0, s>>>(per, p.samples, p.reduction == 2, loss);
+    k_balance_join<<<dim3(p.samples), dim3(1024), 0, s>>>(a, counts, loss, state, p.reduction, (float *)(ws + plan.loss),
+                                                         a.ticket);
 }
 
 void balance_backward(const BalanceProblem &p, const float *state, const float *grad_loss, void *grad, hipStream_t s)
@@ -497,10 +644,11 @@ void balance_backward(const BalanceProblem &p, const float *state, const float *
     const RowShape r = row_shape(p, grad);
     BalanceArgs a = args_of(p);
     a.lanes = r.lanes;
+    a.tile = tile_tokens(p, r);
     cut_tokens(p, 4096, least_tokens(p) / 2, &a.chunk, &a.chunks);
     by_shape(p.type, r, [&](auto l, auto vec, auto nv) {
         k_balance_grad<decltype(l), decltype(vec)::value, decltype(nv)::value>
-            <<<dim3((unsigned)(p.samples * a.chunks)), dim3(kBlock), 0, s>>>(
+            <<<dim3((unsigned)(p.samples * a.chunks)), dim3(kBlock), tile_bytes(p, r), s>>>(
                 a, state, grad_loss, p.reduction == 0, p.reduction == 2 ? 1.0f / (float)p.samples : 1.0f, grad);
     });
 }

@@ -123,7 +123,13 @@ struct Product {
     int group;       // q tiles that a run of workgroups stays within
 };
 
-__device__ __forceinline__ int k_swizzle(int k) { return ((k & 3) | ((k >> 1) & 4)) << 1; }
+// Chunks that row k of a tile with ROWS columns is moved by: a transposing read
+// takes 2 chunks each of k = 8 a .. 8 a + 3 for a = 0 .. 3, which then cover all
+// banks twice (128 columns or more fill them with one row, 64 with two).
+template <int ROWS> __device__ __forceinline__ int k_swizzle(int k)
+{
+    return ROWS >= 128 ? ((k & 3) | ((k >> 1) & 4)) << 1 : (((k >> 1) & 1) | ((k >> 2) & 2)) << 1;
+}
 
 // Byte offset, from the operand's base of a step, of what lane `lane` of load
 // `j` (1 KB of the tile) fetches. With k contiguous the tile holds ROWS rows of
@@ -150,7 +156,7 @@ __device__ __forceinline__ uint32_t tile_offset(const Operand &o, int r0, int j,
     } else {
         constexpr int CH = ROWS / 8;
         const int k = j * (64 / CH) + lane / CH;
-        const int c = (lane % CH) ^ k_swizzle(k);
+        const int c = (lane % CH) ^ k_swizzle<ROWS>(k);
         const int col = min(r0 + c * 8, (o.rows - 1) & ~7);
         return (uint32_t)(min(k, k_left - 1) * o.ld + (col - first_row<KS>(o, r0))) * 2u;
     }
@@ -201,7 +207,7 @@ __device__ __forceinline__ i16x8 fragment(const lds_char *tile, int r0, int i, i
         // a transposing read gives lane i of 16 the column i of 4 rows of 16
         const int k = h * 32 + (lane >> 4) * 8 + ((lane & 15) >> 2);
         const int col = r + (lane & 3) * 4;
-        const lds_char *at = tile + k * (ROWS * 2) + (((col >> 3) ^ k_swizzle(k)) << 4) + ((col & 7) << 1);
+        const lds_char *at = tile + k * (ROWS * 2) + (((col >> 3) ^ k_swizzle<ROWS>(k)) << 4) + ((col & 7) << 1);
         using v4 = __attribute__((address_space(3))) i16x4;
         const i16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((v4 *)at);
         const i16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((v4 *)(at + 4 * ROWS * 2));
@@ -223,6 +229,7 @@ template <int TP_, int TQ_, int WP_, int WQ_, int BUFS_> struct Shape {
 struct Place {
     int p0, q0, sample, split; // where a workgroup's tile starts
     int wp, wq, lane;          // wave within the workgroup
+    lds_char *lds;             // the wave's part of the tiles' memory, free once all waves are done with them
 };
 
 // ELEM: the elements; PLANES: float32 operands in three planes; PK, QK: the
@@ -237,6 +244,7 @@ __global__ __launch_bounds__(S::threads) void k_product(Product a, Finish finish
     at.lane = lane;
     at.wp = wave % S::WP;
     at.wq = wave / S::WP;
+    at.lds = (lds_char *)smem + wave * (S::lds / S::waves);
     {
         // The workgroups of an XCD take a run of tiles; within it, `group` q
         // tiles for one p tile after the other, so that the tiles in flight
@@ -296,6 +304,10 @@ __global__ __launch_bounds__(S::threads) void k_product(Product a, Finish finish
             load_to_lds(rq, oq[j], to + S::TP * 128 + ((wave * S::LQ + j) % (S::TQ / 8)) * 1024);
     };
 
+    // what the finish needs of its rows is on its way during the products
+    typename Finish::template Rows<S> rows;
+    finish.fetch(a, at, rows);
+
     f32x4 acc[S::SP][S::SQ];
 #pragma unroll
     for (int i = 0; i < S::SP; ++i)
@@ -333,10 +345,13 @@ __global__ __launch_bounds__(S::threads) void k_product(Product a, Finish finish
     }
     // lane l holds, of 16 x 16 results, q = l & 15 and p = 4 (l >> 4) .. + 3; with
     // P's k contiguous, of 32 x 16, p = 8 (l >> 4) .. + 7 in two neighbours acc
-    finish.template operator()<ELEM, S>(a, at, acc);
+    finish.template operator()<ELEM, S>(a, at, rows, acc);
 }
 
 // --- what becomes of the results -------------------------------------------
+
+// The class, from a lane's first, of its value i of fragment k (EIGHTS).
+__device__ constexpr int class_of(int k, int i) { return (k >> 1) * 32 + (k & 1) * 4 + i; }
 
 // Forward: per row (q) the maximum and the sum of exp(z - max) over a wave's
 // classes (p), without the target's, whose logit is kept apart. Logits are in
@@ -350,49 +365,63 @@ struct FinishStats {
     float *picked;  // [samples * rows]
     int *ticket;    // cleared for k_ce_rows
     float scale2;
+    template <class S> struct Rows {
+        int target[S::SQ];
+    };
+    template <class S> __device__ __forceinline__ void fetch(const Product &a, const Place &at, Rows<S> &r) const
+    {
+#pragma unroll
+        for (int j = 0; j < S::SQ; ++j) {
+            const int t = at.q0 + at.wq * (S::SQ * 16) + j * 16 + (at.lane & 15);
+            r.target[j] = t < a.q.rows ? target[(int64_t)at.sample * a.q.rows + t] : kIgnored;
+        }
+    }
     template <class ELEM, class S>
-    __device__ __forceinline__ void operator()(const Product &a, const Place &at, f32x4 (&acc)[S::SP][S::SQ]) const
+    __device__ __forceinline__ void operator()(const Product &a, const Place &at, const Rows<S> &r,
+                                               f32x4 (&acc)[S::SP][S::SQ]) const
     {
         if (blockIdx.x == 0 && threadIdx.x == 0)
             *ticket = 0;
         if (scale2 >= 0.0f)
-            reduce<S, true>(a, at, acc);
+            reduce<S, true>(a, at, r, acc);
         else
-            reduce<S, false>(a, at, acc);
+            reduce<S, false>(a, at, r, acc);
     }
     template <class S, bool POSITIVE>
-    __device__ __forceinline__ void reduce(const Product &a, const Place &at, f32x4 (&acc)[S::SP][S::SQ]) const
+    __device__ __forceinline__ void reduce(const Product &a, const Place &at, const Rows<S> &r,
+                                           f32x4 (&acc)[S::SP][S::SQ]) const
     {
         constexpr float none = POSITIVE ? -kInf : kInf;
         const auto further = [](float x, float y) { return POSITIVE ? fmaxf(x, y) : fminf(x, y); };
         const int g = at.lane >> 4;
         const int w0 = at.p0 + at.wp * (S::SP * 16), v0 = w0 + 8 * g;
         const int64_t total = (int64_t)a.samples * a.q.rows;
-        if (w0 + S::SP * 16 > a.p.rows) {
-#pragma unroll
-            for (int k = 0; k < S::SP; ++k)
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    if (v0 + (k >> 1) * 32 + (k & 1) * 4 + i >= a.p.rows)
-#pragma unroll
-                        for (int j = 0; j < S::SQ; ++j)
-                            acc[k][j][i] = none;
-        }
+        const bool edge = w0 + S::SP * 16 > a.p.rows;
 #pragma unroll
         for (int j = 0; j < S::SQ; ++j) {
             const int t = at.q0 + at.wq * (S::SQ * 16) + j * 16 + (at.lane & 15);
             const int64_t row = (int64_t)at.sample * a.q.rows + t;
             const bool in = t < a.q.rows;
-            const int d = (in ? target[row] : kIgnored) - v0;
-            if (__any(d >= 0 && d < S::SP * 16)) {
+            const int d = r.target[j] - v0;
+            if (edge) {
 #pragma unroll
                 for (int k = 0; k < S::SP; ++k)
 #pragma unroll
                     for (int i = 0; i < 4; ++i)
-                        if (d == (k >> 1) * 32 + (k & 1) * 4 + i) {
-                            picked[row] = acc[k][j][i] * scale2;
-                            acc[k][j][i] = none;
-                        }
+                        acc[k][j][i] = v0 + class_of(k, i) >= a.p.rows ? none : acc[k][j][i];
+            }
+            if (__any(d >= 0 && d < S::SP * 16)) {
+                float z = 0.0f;
+#pragma unroll
+                for (int k = 0; k < S::SP; ++k)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const bool hit = d == class_of(k, i);
+                        z = hit ? acc[k][j][i] : z;
+                        acc[k][j][i] = hit ? none : acc[k][j][i];
+                    }
+                if (d >= 0 && d < S::SP * 16 && (d & 31) < 8) // the lane's own classes
+                    picked[row] = z * scale2;
             }
             float m = none;
 #pragma unroll
@@ -414,6 +443,7 @@ struct FinishStats {
             sum += __shfl_xor(sum, 32);
             if (in && g == 0)
                 part[(int64_t)(at.p0 / S::TP * S::WP + at.wp) * total + row] = make_float2(top, sum);
+            __builtin_amdgcn_sched_barrier(0); // rows side by side would not fit the registers
         }
     }
 };
@@ -442,21 +472,35 @@ template <bool PLANES> struct FinishGrad {
     int64_t plane;
     float scale2;
     int rows_pad, ld, class0;
+    template <class S> struct Rows {
+        CeCoef coef[S::SQ];
+        int target[S::SQ];
+    };
+    template <class S> __device__ __forceinline__ void fetch(const Product &a, const Place &at, Rows<S> &r) const
+    {
+#pragma unroll
+        for (int j = 0; j < S::SQ; ++j) {
+            const int t = at.q0 + at.wq * (S::SQ * 16) + j * 16 + (at.lane & 15);
+            const int64_t row = row0 + (int64_t)at.sample * a.q.rows + t;
+            r.coef[j] = CeCoef{0.0f, 0.0f, 0.0f, 0.0f};
+            r.target[j] = kIgnored;
+            if (t < a.q.rows) {
+                r.coef[j] = coef[row];
+                r.target[j] = target[row] - class0;
+            }
+        }
+    }
     template <class ELEM, class S>
-    __device__ __forceinline__ void operator()(const Product &a, const Place &at, f32x4 (&acc)[S::SP][S::SQ]) const
+    __device__ __forceinline__ void operator()(const Product &a, const Place &at, const Rows<S> &r,
+                                               f32x4 (&acc)[S::SP][S::SQ]) const
     {
         const int w0 = at.p0 + at.wp * (S::SP * 16), v0 = w0 + 8 * (at.lane >> 4);
         const bool edge = w0 + S::SP * 16 > a.p.rows;
 #pragma unroll
         for (int j = 0; j < S::SQ; ++j) {
             const int t = at.q0 + at.wq * (S::SQ * 16) + j * 16 + (at.lane & 15);
-            const int64_t row = row0 + (int64_t)at.sample * a.q.rows + t;
-            CeCoef c{0.0f, 0.0f, 0.0f, 0.0f};
-            int d = kIgnored;
-            if (t < a.q.rows) {
-                c = coef[row];
-                d = target[row] - class0 - v0;
-            }
+            const CeCoef c = r.coef[j];
+            const int d = r.target[j] - v0;
             if (__any(c.fac == 0.0f)) {
 #pragma unroll
                 for (int k = 0; k < S::SP; ++k)
@@ -474,16 +518,14 @@ template <bool PLANES> struct FinishGrad {
                 for (int k = 0; k < S::SP; ++k)
 #pragma unroll
                     for (int i = 0; i < 4; ++i)
-                        if (d == (k >> 1) * 32 + (k & 1) * 4 + i)
-                            acc[k][j][i] = c.at_target;
+                        acc[k][j][i] = d == class_of(k, i) ? c.at_target : acc[k][j][i];
             }
             if (edge) {
 #pragma unroll
                 for (int k = 0; k < S::SP; ++k)
 #pragma unroll
                     for (int i = 0; i < 4; ++i)
-                        if (v0 + (k >> 1) * 32 + (k & 1) * 4 + i >= a.p.rows)
-                            acc[k][j][i] = 0.0f;
+                        acc[k][j][i] = v0 + class_of(k, i) >= a.p.rows ? 0.0f : acc[k][j][i];
             }
             uint16_t *to = g + ((int64_t)at.sample * rows_pad + t) * ld + v0;
 #pragma unroll
@@ -509,6 +551,7 @@ template <bool PLANES> struct FinishGrad {
                 }
                 *(i16x8 *)(to + k * 16) = p0;
             }
+            __builtin_amdgcn_sched_barrier(0); // rows side by side would not fit the registers
         }
     }
 };
@@ -534,31 +577,78 @@ template <class OUT> struct FinishStore {
     const CeTop *top;   // grad_w: the largest unit
     float inv_unit;     // 1 / ELEM::kUnit
     int64_t sample;     // elements from one sample's output to the next
+    template <class S> struct Rows {
+        float unit[S::SQ];
+    };
+    template <class S> __device__ __forceinline__ void fetch(const Product &a, const Place &at, Rows<S> &r) const
+    {
+#pragma unroll
+        for (int j = 0; j < S::SQ; ++j) {
+            const int q = min(at.q0 + at.wq * (S::SQ * 16) + j * 16 + (at.lane & 15), a.q.rows - 1);
+            r.unit[j] = coef ? coef[(int64_t)at.sample * a.q.rows + q].unit : top->top;
+        }
+    }
     template <class ELEM, class S>
-    __device__ __forceinline__ void operator()(const Product &a, const Place &at, f32x4 (&acc)[S::SP][S::SQ]) const
+    __device__ __forceinline__ void operator()(const Product &a, const Place &at, const Rows<S> &r,
+                                               f32x4 (&acc)[S::SP][S::SQ]) const
+    {
+        if (a.p.rows % 4 == 0)
+            direct<S>(a, at, r, acc);
+        else
+            staged<S>(a, at, r, acc);
+    }
+    // Four neighbours at a time.
+    template <class S>
+    __device__ __forceinline__ void direct(const Product &a, const Place &at, const Rows<S> &r,
+                                           f32x4 (&acc)[S::SP][S::SQ]) const
     {
         const int p0 = at.p0 + at.wp * (S::SP * 16) + 4 * (at.lane >> 4);
-        const bool wide = a.p.rows % 4 == 0;
 #pragma unroll
         for (int j = 0; j < S::SQ; ++j) {
             const int q = at.q0 + at.wq * (S::SQ * 16) + j * 16 + (at.lane & 15);
             if (q >= a.q.rows)
                 continue;
-            const float f = (coef ? coef[(int64_t)at.sample * a.q.rows + q].unit : top->top) * inv_unit;
+            const float f = r.unit[j] * inv_unit;
             const int64_t to = at.sample * sample + (int64_t)q * a.p.rows;
 #pragma unroll
             for (int k = 0; k < S::SP; ++k) {
                 const int p = p0 + k * 16;
-                if (wide) {
-                    if (p < a.p.rows)
-                        put4<OUT>(out, to + p, acc[k][j] * f);
-                } else {
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        if (p + i < a.p.rows)
-                            put<OUT>(out, to + p + i, acc[k][j][i] * f);
-                }
+                if (p < a.p.rows)
+                    put4<OUT>(out, to + p, acc[k][j] * f);
             }
+        }
+    }
+    // Rows that start at any element: 16 of them pass through shared memory, from
+    // where a wave writes each row's neighbours together (1003 columns of half
+    // precision, 2-byte stores of lanes 8 bytes apart: 163 us for 25000 rows).
+    template <class S>
+    __device__ __forceinline__ void staged(const Product &a, const Place &at, const Rows<S> &r,
+                                           f32x4 (&acc)[S::SP][S::SQ]) const
+    {
+        constexpr int W = S::SP * 16, LD = W + 4; // a row of the wave's results, in float32
+        static_assert(16 * LD * 4 <= S::lds / S::waves, "a wave's part of the tiles holds 16 rows");
+        wait_lds_and_meet();
+        auto *row = (__attribute__((address_space(3))) float *)at.lds;
+        const int p0 = at.p0 + at.wp * W, q0 = at.q0 + at.wq * (S::SQ * 16);
+#pragma unroll
+        for (int j = 0; j < S::SQ; ++j) {
+            const float f = r.unit[j] * inv_unit;
+#pragma unroll
+            for (int k = 0; k < S::SP; ++k)
+                *(__attribute__((address_space(3))) f32x4 *)(row + (at.lane & 15) * LD + k * 16 + 4 * (at.lane >> 4)) =
+                    acc[k][j] * f;
+            __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront", "local");
+            __builtin_amdgcn_wave_barrier();
+            __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront", "local");
+            const int n = min(16, a.q.rows - q0 - j * 16);
+            for (int i = at.lane; i < n * W; i += 64) {
+                const int p = p0 + i % W;
+                if (p < a.p.rows)
+                    put<OUT>(out, at.sample * sample + (int64_t)(q0 + j * 16 + i / W) * a.p.rows + p, row[i / W * LD + i % W]);
+            }
+            __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront", "local");
+            __builtin_amdgcn_wave_barrier();
+            __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront", "local");
         }
     }
 };
@@ -570,8 +660,11 @@ struct FinishPart {
     int64_t split, sample; // elements from one part, one sample to the next
     int ld;                // p rows up to a multiple of 4
     bool add;
+    template <class S> struct Rows {};
+    template <class S> __device__ __forceinline__ void fetch(const Product &, const Place &, Rows<S> &) const {}
     template <class ELEM, class S>
-    __device__ __forceinline__ void operator()(const Product &a, const Place &at, f32x4 (&acc)[S::SP][S::SQ]) const
+    __device__ __forceinline__ void operator()(const Product &a, const Place &at, const Rows<S> &,
+                                               f32x4 (&acc)[S::SP][S::SQ]) const
     {
         const int p0 = at.p0 + at.wp * (S::SP * 16) + 4 * (at.lane >> 4);
 #pragma unroll
@@ -780,10 +873,13 @@ __global__ __launch_bounds__(kBlock) void k_ce_rows(const float2 *part, int part
             s.sum += sl[k].sum;
             s.count += sl[k].count;
         }
-        sums[blockIdx.x] = s;
-        __threadfence();
-        is_last = atomicAdd(ticket, 1) == (int)gridDim.x - 1;
-        __threadfence();
+        // device-scope stores and loads go past the XCDs' own L2s, so a wait for
+        // the stores is all the order that the ticket needs (a release fence
+        // would write the whole L2 back: 10 us more for 512 workgroups)
+        __hip_atomic_store(&sums[blockIdx.x].sum, s.sum, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        __hip_atomic_store(&sums[blockIdx.x].count, s.count, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        is_last = __hip_atomic_fetch_add(ticket, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (int)gridDim.x - 1;
     }
     __syncthreads();
     if (!is_last)
@@ -793,8 +889,8 @@ __global__ __launch_bounds__(kBlock) void k_ce_rows(const float2 *part, int part
     double a = 0.0;
     int64_t c = 0;
     for (unsigned i = threadIdx.x; i < gridDim.x; i += kBlock) {
-        a += sums[i].sum;
-        c += sums[i].count;
+        a += __hip_atomic_load(&sums[i].sum, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        c += __hip_atomic_load(&sums[i].count, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     }
     a = wave_sum(a);
     for (int o = 32; o > 0; o >>= 1)
@@ -946,26 +1042,53 @@ __global__ __launch_bounds__(kBlock) void k_ce_join(const float *part, int split
 // ---------------------------------------------------------------------------
 
 using Large = Shape<256, 256, 2, 4, 2>;
+using Tall = Shape<256, 256, 4, 2, 2>;
 using Medium = Shape<128, 128, 2, 2, 2>;
 using Narrow = Shape<128, 16, 4, 1, 4>;
+using Thin = Shape<64, 128, 2, 2, 2>;
 
 int ceil_to(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
 int64_t pad_to(int64_t a, int64_t b) { return (a + b - 1) / b * b; }
 
-enum class Kind { large, medium, narrow };
+enum class Kind { large, tall, medium, narrow, thin };
 
-// The tile of a product of `classes` by `rows` results.
-Kind choose(int64_t p, int64_t q, int64_t batches, bool narrow_ok)
+// Whether 256 x 256 tiles, one a compute unit, end before 128 x 128 ones, two a
+// compute unit: rounds of each, a round of the latter taking 0.54 of the former's
+// time (8192 x 8192 x 1024: 118 us against 134 in four rounds and eight).
+bool large_tiles(int64_t p, int64_t q, int64_t batches)
 {
-    if (narrow_ok && q <= 16)
-        return Kind::narrow;
-    if (ceil_to(p, 256) * (int64_t)ceil_to(q, 256) * batches >= 256)
-        return Kind::large;
-    return Kind::medium;
+    const int64_t large = ceil_to(p, 256) * (int64_t)ceil_to(q, 256) * batches;
+    const int64_t medium = ceil_to(p, 128) * (int64_t)ceil_to(q, 128) * batches;
+    return ceil_to(large, 256) <= 0.54 * ceil_to(medium, 512);
 }
-int tile_p(Kind k) { return k == Kind::large ? 256 : 128; }
-int tile_q(Kind k) { return k == Kind::large ? 256 : k == Kind::medium ? 128 : 16; }
-int waves_p(Kind k) { return k == Kind::narrow ? Narrow::WP : 2; }
+
+// The tile of a product of p classes and q rows, `batches` of them, of `steps`
+// steps: 16 rows where there are no more (one row of 131072 x 4096: w streams at
+// 6 TB/s). Waves of 64 x 128 results read fewer bytes from the tiles than their
+// transpose (131072 x 8192 x 4096: 6.52 against 6.78 ms), but reduce over the
+// classes four times as often (16384 x 4096 x 256: 785 against 697 us).
+Kind choose(int64_t p, int64_t q, int64_t batches, int64_t steps)
+{
+    if (q <= 16)
+        return Kind::narrow;
+    if (!large_tiles(p, q, batches))
+        return Kind::medium;
+    return steps >= 32 ? Kind::tall : Kind::large;
+}
+// The same for the gradients, whose p axis is the features: no more than 64 of
+// them would leave half of a 128 wide tile empty.
+Kind choose_grad(int64_t dim, int64_t q, int64_t batches, bool narrow)
+{
+    if (narrow && q <= 16)
+        return Kind::narrow;
+    if (dim <= 64)
+        return Kind::thin;
+    return large_tiles(dim, q, batches) ? Kind::tall : Kind::medium;
+}
+bool is_large(Kind k) { return k == Kind::large || k == Kind::tall; }
+int tile_p(Kind k) { return is_large(k) ? 256 : k == Kind::thin ? 64 : 128; }
+int tile_q(Kind k) { return is_large(k) ? 256 : k == Kind::narrow ? 16 : 128; }
+int waves_p(Kind k) { return k == Kind::narrow ? Narrow::WP : k == Kind::tall ? Tall::WP : 2; }
 
 template <class ELEM, bool PLANES, bool PK, bool QK, class S, class F>
 void launch_shape(Product a, int64_t cover_p, int64_t cover_q, const F &f, hipStream_t s)
@@ -982,11 +1105,17 @@ void launch_shape(Product a, int64_t cover_p, int64_t cover_q, const F &f, hipSt
 template <class ELEM, bool PLANES, bool PK, bool QK, class F>
 void launch_product(Kind kind, const Product &a, int64_t cover_p, int64_t cover_q, const F &f, hipStream_t s)
 {
-    if (kind == Kind::large)
-        launch_shape<ELEM, PLANES, PK, QK, Large>(a, cover_p, cover_q, f, s);
+    if (kind == Kind::tall)
+        launch_shape<ELEM, PLANES, PK, QK, Tall>(a, cover_p, cover_q, f, s);
     else if (kind == Kind::medium)
         launch_shape<ELEM, PLANES, PK, QK, Medium>(a, cover_p, cover_q, f, s);
-    else if constexpr (!QK)
+    else if (kind == Kind::large) {
+        if constexpr (!PK)
+            launch_shape<ELEM, PLANES, PK, QK, Large>(a, cover_p, cover_q, f, s);
+    } else if (kind == Kind::thin) {
+        if constexpr (PK)
+            launch_shape<ELEM, PLANES, PK, QK, Thin>(a, cover_p, cover_q, f, s);
+    } else if constexpr (!QK)
         launch_shape<ELEM, PLANES, PK, QK, Narrow>(a, cover_p, cover_q, f, s);
 }
 
@@ -1002,6 +1131,7 @@ struct Offsets {
 
 bool aligned16(const void *p) { return ((uintptr_t)p & 15) == 0; }
 int planes(const CeProblem &p) { return p.type == ElemType::f32 ? 3 : 1; }
+int dim_steps(const CeProblem &p) { return ceil_to(p.dim, kCeStep) * (planes(p) == 3 ? kPlaneProducts : 1); }
 int64_t all_rows(const CeProblem &p) { return (int64_t)p.samples * p.rows; }
 
 // x is copied where its rows are no whole steps (the copy's zeros are what ends
@@ -1073,15 +1203,15 @@ template <class F> void by_type(ElemType t, F f)
 
 // Threads of k_ce_rows a row: with few rows, as many as it takes to have the
 // parts' loads in flight together (one row of 131072 classes, 4096 parts: 16
-// threads 105 us).
-static int row_threads(int64_t n) { return n >= 4096 ? 16 : kBlock; }
+// threads 105 us, 256 threads 5.5 us).
+static int row_threads(int64_t n) { return n >= 256 ? 16 : kBlock; }
 
 CeForwardPlan ce_plan_forward(const CeProblem &p)
 {
     CeForwardPlan f{};
     choose_packs(p, &f.pack_x, &f.pack_w);
     f.dim_pad = (int)pad_to(p.dim, kCeStep);
-    const Kind kind = choose(p.classes, p.rows, p.samples, true);
+    const Kind kind = choose(p.classes, p.rows, p.samples, dim_steps(p));
     f.parts = ceil_to(p.classes, tile_p(kind)) * waves_p(kind);
     const int64_t n = all_rows(p);
     Offsets o;
@@ -1122,7 +1252,7 @@ void ce_forward(const CeProblem &p, const CeForwardPlan &plan, uint8_t *ws, floa
         a.steps = plan.dim_pad / kCeStep;
         a.samples = p.samples;
         a.splits = 1;
-        launch_product<ELEM, decltype(cut)::value, false, false>(choose(p.classes, p.rows, p.samples, true), a,
+        launch_product<ELEM, decltype(cut)::value, false, false>(choose(p.classes, p.rows, p.samples, dim_steps(p)), a,
                                                                  p.classes, p.rows,
                                                                  FinishStats{target, part, picked, ticket, scale2_of(p)}, s);
     });
@@ -1136,17 +1266,20 @@ void ce_forward(const CeProblem &p, const CeForwardPlan &plan, uint8_t *ws, floa
 
 namespace {
 
-// The piece of the logits' gradient that exists at a time: what stays in the
-// 256 MB last-level cache between the product that writes it and the two that
-// read it.
-constexpr int64_t kPieceBytes = (int64_t)128 << 20;
+// The piece of the logits' gradient that exists at a time: about what the 256 MB
+// last-level cache keeps between the product that writes it and the two that
+// read it. Smaller pieces are more launches, each with a tail (64, 128, 256, 512
+// MB: 16 x 4096 x 16384 x 256 4.21, 3.72, 3.45, 3.56 ms; 32 x 2048 x 2048 x 64
+// float32 1.37, 1.20, 1.12, 1.33 ms).
+constexpr int64_t kPieceBytes = (int64_t)256 << 20;
 
-// Parts of a sum of `steps` steps so that a product of few tiles fills the card.
-int choose_splits(int64_t tiles, int64_t steps)
+// Parts of a sum of `steps` steps so that a product of few tiles fills the card,
+// each of at least `least` steps: a part's results are written and read again.
+int choose_splits(int64_t tiles, int64_t steps, int least)
 {
     if (tiles >= 256)
         return 1;
-    return (int)std::max<int64_t>(1, std::min<int64_t>({512 / std::max<int64_t>(tiles, 1), steps / 8, 64}));
+    return (int)std::max<int64_t>(1, std::min<int64_t>({512 / std::max<int64_t>(tiles, 1), steps / least, 64}));
 }
 
 } // namespace
@@ -1169,11 +1302,12 @@ CeBackwardPlan ce_plan_backward(const CeProblem &p, bool want_x, bool want_w)
         b.piece_classes = (int)std::min<int64_t>(p.classes, pad_to(ceil_to(p.classes, pieces), 256));
     }
     b.ld_g = (int)pad_to(b.piece_classes, kCeStep);
-    const Kind kx = choose(p.dim, p.rows, b.piece_samples, true), kw = choose(p.dim, b.piece_classes, b.piece_samples, false);
+    const int least = p.type == ElemType::f32 ? 2 : 8; // a float32 step is six
+    const Kind kx = choose_grad(p.dim, p.rows, b.piece_samples, true), kw = choose_grad(p.dim, b.piece_classes, b.piece_samples, false);
     b.split_x = choose_splits((int64_t)ceil_to(p.dim, tile_p(kx)) * ceil_to(p.rows, tile_q(kx)) * b.piece_samples,
-                              b.ld_g / kCeStep);
+                              b.ld_g / kCeStep, least);
     b.split_w = choose_splits((int64_t)ceil_to(p.dim, tile_p(kw)) * ceil_to(b.piece_classes, tile_q(kw)) * b.piece_samples,
-                              b.rows_pad / kCeStep);
+                              b.rows_pad / kCeStep, least);
     b.sum_x = b.split_x > 1 || b.piece_classes < p.classes;
     const int64_t ld = pad_to(p.dim, 4);
     Offsets o;
@@ -1244,7 +1378,7 @@ void ce_backward(const CeProblem &p, const CeBackwardPlan &plan, uint8_t *ws, co
                     a.splits = 1;
                     const int64_t r0 = (int64_t)s0 * p.rows;
                     launch_product<ELEM, PLANES, false, false>(
-                        choose(nc, p.rows, ns, true), a, nc_pad, plan.rows_pad,
+                        choose(nc, p.rows, ns, dim_steps(p)), a, nc_pad, plan.rows_pad,
                         FinishGrad<PLANES>{target, coef, r0, g, plane_g, scale2_of(p), plan.rows_pad, plan.ld_g, c0}, s);
                 }
                 Operand G;
@@ -1263,7 +1397,7 @@ void ce_backward(const CeProblem &p, const CeBackwardPlan &plan, uint8_t *ws, co
                     a.q.k = nc_pad;
                     a.steps = nc_pad / kCeStep;
                     a.samples = ns;
-                    const Kind kind = choose(p.dim, p.rows, plan.piece_samples, true);
+                    const Kind kind = choose_grad(p.dim, p.rows, plan.piece_samples, true);
                     if (plan.sum_x) {
                         a.splits = plan.split_x;
                         const int64_t sample = (int64_t)p.rows * ld, split = plan.piece_samples * sample;
@@ -1293,7 +1427,7 @@ void ce_backward(const CeProblem &p, const CeBackwardPlan &plan, uint8_t *ws, co
                     a.steps = plan.rows_pad / kCeStep;
                     a.samples = ns;
                     a.splits = plan.split_w;
-                    const Kind kind = choose(p.dim, plan.piece_classes, plan.piece_samples, false);
+                    const Kind kind = choose_grad(p.dim, plan.piece_classes, plan.piece_samples, false);
                     const int64_t sample = (int64_t)p.classes * p.dim;
                     void *to = (uint8_t *)grad_w + (s0 * sample + (int64_t)c0 * p.dim) * elem_size(p.type);
                     if (plan.split_w > 1) {
