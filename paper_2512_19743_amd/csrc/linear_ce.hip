@@ -215,9 +215,13 @@ __device__ __forceinline__ i16x8 fragment(const lds_char *tile, int r0, int i, i
     }
 }
 
-// The tile shapes. A workgroup takes TP x TQ results, its waves WP x WQ of them.
-template <int TP_, int TQ_, int WP_, int WQ_, int BUFS_> struct Shape {
+// The tile shapes. A workgroup takes TP x TQ results, its waves WP x WQ of them,
+// with BUFS steps' tiles in shared memory. WOVEN: the fragments of the next half
+// step are read between the matrix instructions of this one.
+template <int TP_, int TQ_, int WP_, int WQ_, int BUFS_, bool WOVEN_ = false> struct Shape {
     static constexpr int TP = TP_, TQ = TQ_, WP = WP_, WQ = WQ_, BUFS = BUFS_;
+    static constexpr bool WOVEN = WOVEN_;
+    static_assert(!WOVEN || BUFS == 2, "two tiles in turn");
     static constexpr int waves = WP * WQ, threads = 64 * waves;
     static constexpr int SP = TP / WP / 16, SQ = TQ / WQ / 16; // 16 x 16 results of a wave
     static constexpr int stage = (TP + TQ) * 128;
@@ -315,32 +319,89 @@ __global__ __launch_bounds__(S::threads) void k_product(Product a, Finish finish
         for (int j = 0; j < S::SQ; ++j)
             acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 
-    for (int i = 0; i < S::BUFS - 1 && i < total; ++i)
-        load(i);
-    for (int i = 0; i < total; ++i) {
-        // this step's tile has arrived once at most the later steps' loads are out
-        if (i + S::BUFS - 2 < total)
-            wait_loads<(S::BUFS - 2) * (S::LP + S::LQ)>();
-        else
-            wait_loads<0>();
-        wait_lds_and_meet(); // also: every wave has read the tile that the next load overwrites
-        if (i + S::BUFS - 1 < total)
-            load(i + S::BUFS - 1);
+    const auto read = [&](int i, int h, i16x8 (&fp)[S::SP], i16x8 (&fq)[S::SQ]) {
         const lds_char *tp = (const lds_char *)smem + (i % S::BUFS) * S::stage, *tq = tp + S::TP * 128;
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            i16x8 fp[S::SP], fq[S::SQ];
+        for (int j = 0; j < S::SQ; ++j)
+            fq[j] = fragment<S::TQ, QK, false>(tq, at.wq * (S::SQ * 16), j, h, lane);
+#pragma unroll
+        for (int k = 0; k < S::SP; ++k)
+            fp[k] = fragment<S::TP, PK, !PK>(tp, at.wp * (S::SP * 16), k, h, lane);
+    };
+    const auto multiply = [&](const i16x8 (&fp)[S::SP], const i16x8 (&fq)[S::SQ]) {
+#pragma unroll
+        for (int k = 0; k < S::SP; ++k)
 #pragma unroll
             for (int j = 0; j < S::SQ; ++j)
-                fq[j] = fragment<S::TQ, QK, false>(tq, at.wq * (S::SQ * 16), j, h, lane);
+                acc[k][j] = ELEM::mma(fp[k], fq[j], acc[k][j]);
+    };
+
+    // Every barrier says two things: a step's tile has arrived (each wave has
+    // waited for its own loads), and every wave has read the tile whose place the
+    // next loads take.
+    if constexpr (S::WOVEN) {
+        // With one workgroup a compute unit, its two waves a SIMD meet at every
+        // barrier, and fragments read right after it leave the matrix cores idle
+        // in both. So a half step's fragments are read one half step ahead, a read
+        // after every one or two matrix instructions, and the barrier stands in
+        // the middle of a step, with a half step's instructions ready behind it
+        // (8192 x 131072 x 4096: 1.30 -> 1.43 PFLOP/s; with the reads ahead but
+        // not woven in 1.39).
+        constexpr int reads = S::SP * (PK ? 2 : 1) + S::SQ * (QK ? 2 : 1), products = S::SP * S::SQ;
+        const auto weave = [] {
 #pragma unroll
-            for (int k = 0; k < S::SP; ++k)
-                fp[k] = fragment<S::TP, PK, !PK>(tp, at.wp * (S::SP * 16), k, h, lane);
+            for (int r = 0; r < reads; ++r) {
+                __builtin_amdgcn_sched_group_barrier(0x100, 1, 0); // a read from shared memory
+                __builtin_amdgcn_sched_group_barrier(0x008, products / reads, 0); // matrix instructions
+            }
+            __builtin_amdgcn_sched_group_barrier(0x008, products, 0);
+        };
+        static_assert(products >= reads, "");
+        if (total > 0) {
+            load(0);
+            if (total > 1) {
+                load(1);
+                wait_loads<S::LP + S::LQ>();
+            } else {
+                wait_loads<0>();
+            }
+            wait_lds_and_meet();
+            i16x8 p0[S::SP], q0[S::SQ], p1[S::SP], q1[S::SQ];
+            read(0, 0, p0, q0);
+            for (int i = 0; i < total; ++i) {
+                __builtin_amdgcn_sched_barrier(0);
+                read(i, 1, p1, q1);
+                multiply(p0, q0);
+                weave();
+                __builtin_amdgcn_sched_barrier(0);
+                wait_loads<0>();
+                wait_lds_and_meet();
+                if (i + 2 < total)
+                    load(i + 2);
+                __builtin_amdgcn_sched_barrier(0);
+                read(i + 1 < total ? i + 1 : i, 0, p0, q0); // the last one's is not used
+                multiply(p1, q1);
+                weave();
+            }
+        }
+    } else {
+        for (int i = 0; i < S::BUFS - 1 && i < total; ++i)
+            load(i);
+        for (int i = 0; i < total; ++i) {
+            // this step's tile has arrived once at most the later steps' loads are out
+            if (i + S::BUFS - 2 < total)
+                wait_loads<(S::BUFS - 2) * (S::LP + S::LQ)>();
+            else
+                wait_loads<0>();
+            wait_lds_and_meet();
+            if (i + S::BUFS - 1 < total)
+                load(i + S::BUFS - 1);
 #pragma unroll
-            for (int k = 0; k < S::SP; ++k)
-#pragma unroll
-                for (int j = 0; j < S::SQ; ++j)
-                    acc[k][j] = ELEM::mma(fp[k], fq[j], acc[k][j]);
+            for (int h = 0; h < 2; ++h) {
+                i16x8 fp[S::SP], fq[S::SQ];
+                read(i, h, fp, fq);
+                multiply(fp, fq);
+            }
         }
     }
     // lane l holds, of 16 x 16 results, q = l & 15 and p = 4 (l >> 4) .. + 3; with
@@ -473,7 +534,7 @@ template <bool PLANES> struct FinishGrad {
     float scale2;
     int rows_pad, ld, class0;
     template <class S> struct Rows {
-        CeCoef coef[S::SQ];
+        float top[S::SQ], fac[S::SQ];
         int target[S::SQ];
     };
     template <class S> __device__ __forceinline__ void fetch(const Product &a, const Place &at, Rows<S> &r) const
@@ -482,10 +543,11 @@ template <bool PLANES> struct FinishGrad {
         for (int j = 0; j < S::SQ; ++j) {
             const int t = at.q0 + at.wq * (S::SQ * 16) + j * 16 + (at.lane & 15);
             const int64_t row = row0 + (int64_t)at.sample * a.q.rows + t;
-            r.coef[j] = CeCoef{0.0f, 0.0f, 0.0f, 0.0f};
+            r.top[j] = r.fac[j] = 0.0f;
             r.target[j] = kIgnored;
             if (t < a.q.rows) {
-                r.coef[j] = coef[row];
+                r.top[j] = coef[row].top;
+                r.fac[j] = coef[row].fac;
                 r.target[j] = target[row] - class0;
             }
         }
@@ -499,26 +561,28 @@ template <bool PLANES> struct FinishGrad {
 #pragma unroll
         for (int j = 0; j < S::SQ; ++j) {
             const int t = at.q0 + at.wq * (S::SQ * 16) + j * 16 + (at.lane & 15);
-            const CeCoef c = r.coef[j];
+            const float top = r.top[j], fac = r.fac[j];
             const int d = r.target[j] - v0;
-            if (__any(c.fac == 0.0f)) {
+            if (__any(fac == 0.0f)) {
 #pragma unroll
                 for (int k = 0; k < S::SP; ++k)
 #pragma unroll
                     for (int i = 0; i < 4; ++i)
-                        acc[k][j][i] = c.fac == 0.0f ? 0.0f : acc[k][j][i];
+                        acc[k][j][i] = fac == 0.0f ? 0.0f : acc[k][j][i];
             }
 #pragma unroll
             for (int k = 0; k < S::SP; ++k)
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
-                    acc[k][j][i] = c.fac * __builtin_amdgcn_exp2f(__builtin_fmaf(acc[k][j][i], scale2, -c.top));
-            if (__any(d >= 0 && d < S::SP * 16)) {
+                    acc[k][j][i] = fac * __builtin_amdgcn_exp2f(__builtin_fmaf(acc[k][j][i], scale2, -top));
+            const bool here = d >= 0 && d < S::SP * 16;
+            if (__any(here)) {
+                const float mine = here ? coef[row0 + (int64_t)at.sample * a.q.rows + t].at_target : 0.0f;
 #pragma unroll
                 for (int k = 0; k < S::SP; ++k)
 #pragma unroll
                     for (int i = 0; i < 4; ++i)
-                        acc[k][j][i] = d == class_of(k, i) ? c.at_target : acc[k][j][i];
+                        acc[k][j][i] = d == class_of(k, i) ? mine : acc[k][j][i];
             }
             if (edge) {
 #pragma unroll
@@ -577,29 +641,26 @@ template <class OUT> struct FinishStore {
     const CeTop *top;   // grad_w: the largest unit
     float inv_unit;     // 1 / ELEM::kUnit
     int64_t sample;     // elements from one sample's output to the next
-    template <class S> struct Rows {
-        float unit[S::SQ];
-    };
-    template <class S> __device__ __forceinline__ void fetch(const Product &a, const Place &at, Rows<S> &r) const
+    template <class S> struct Rows {};
+    template <class S> __device__ __forceinline__ void fetch(const Product &, const Place &, Rows<S> &) const {}
+    template <class ELEM, class S>
+    __device__ __forceinline__ void operator()(const Product &a, const Place &at, const Rows<S> &,
+                                               f32x4 (&acc)[S::SP][S::SQ]) const
     {
+        float unit[S::SQ];
 #pragma unroll
         for (int j = 0; j < S::SQ; ++j) {
             const int q = min(at.q0 + at.wq * (S::SQ * 16) + j * 16 + (at.lane & 15), a.q.rows - 1);
-            r.unit[j] = coef ? coef[(int64_t)at.sample * a.q.rows + q].unit : top->top;
+            unit[j] = (coef ? coef[(int64_t)at.sample * a.q.rows + q].unit : top->top) * inv_unit;
         }
-    }
-    template <class ELEM, class S>
-    __device__ __forceinline__ void operator()(const Product &a, const Place &at, const Rows<S> &r,
-                                               f32x4 (&acc)[S::SP][S::SQ]) const
-    {
         if (a.p.rows % 4 == 0)
-            direct<S>(a, at, r, acc);
+            direct<S>(a, at, unit, acc);
         else
-            staged<S>(a, at, r, acc);
+            staged<S>(a, at, unit, acc);
     }
     // Four neighbours at a time.
     template <class S>
-    __device__ __forceinline__ void direct(const Product &a, const Place &at, const Rows<S> &r,
+    __device__ __forceinline__ void direct(const Product &a, const Place &at, const float (&unit)[S::SQ],
                                            f32x4 (&acc)[S::SP][S::SQ]) const
     {
         const int p0 = at.p0 + at.wp * (S::SP * 16) + 4 * (at.lane >> 4);
@@ -608,7 +669,7 @@ template <class OUT> struct FinishStore {
             const int q = at.q0 + at.wq * (S::SQ * 16) + j * 16 + (at.lane & 15);
             if (q >= a.q.rows)
                 continue;
-            const float f = r.unit[j] * inv_unit;
+            const float f = unit[j];
             const int64_t to = at.sample * sample + (int64_t)q * a.p.rows;
 #pragma unroll
             for (int k = 0; k < S::SP; ++k) {
@@ -622,7 +683,7 @@ template <class OUT> struct FinishStore {
     // where a wave writes each row's neighbours together (1003 columns of half
     // precision, 2-byte stores of lanes 8 bytes apart: 163 us for 25000 rows).
     template <class S>
-    __device__ __forceinline__ void staged(const Product &a, const Place &at, const Rows<S> &r,
+    __device__ __forceinline__ void staged(const Product &a, const Place &at, const float (&unit)[S::SQ],
                                            f32x4 (&acc)[S::SP][S::SQ]) const
     {
         constexpr int W = S::SP * 16, LD = W + 4; // a row of the wave's results, in float32
@@ -632,7 +693,7 @@ template <class OUT> struct FinishStore {
         const int p0 = at.p0 + at.wp * W, q0 = at.q0 + at.wq * (S::SQ * 16);
 #pragma unroll
         for (int j = 0; j < S::SQ; ++j) {
-            const float f = r.unit[j] * inv_unit;
+            const float f = unit[j];
 #pragma unroll
             for (int k = 0; k < S::SP; ++k)
                 *(__attribute__((address_space(3))) f32x4 *)(row + (at.lane & 15) * LD + k * 16 + 4 * (at.lane >> 4)) =
@@ -1041,8 +1102,8 @@ __global__ __launch_bounds__(kBlock) void k_ce_join(const float *part, int split
 // host
 // ---------------------------------------------------------------------------
 
-using Large = Shape<256, 256, 2, 4, 2>;
-using Tall = Shape<256, 256, 4, 2, 2>;
+using Large = Shape<256, 256, 2, 4, 2, true>; // products over the features: fewer reductions over the classes
+using Tall = Shape<256, 256, 4, 2, 2, true>;  // the gradients' (8192 x 4096 x 8192: 386 us; its transpose 394)
 using Medium = Shape<128, 128, 2, 2, 2>;
 using Narrow = Shape<128, 16, 4, 1, 4>;
 using Thin = Shape<64, 128, 2, 2, 2>;
@@ -1050,30 +1111,25 @@ using Thin = Shape<64, 128, 2, 2, 2>;
 int ceil_to(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
 int64_t pad_to(int64_t a, int64_t b) { return (a + b - 1) / b * b; }
 
-enum class Kind { large, tall, medium, narrow, thin };
+enum class Kind { large, medium, narrow, thin };
 
 // Whether 256 x 256 tiles, one a compute unit, end before 128 x 128 ones, two a
-// compute unit: rounds of each, a round of the latter taking 0.54 of the former's
-// time (8192 x 8192 x 1024: 118 us against 134 in four rounds and eight).
+// compute unit: rounds of each, a round of the latter taking 0.58 of the former's
+// time (8192 x 8192 x 1024: 116 us against 134 in four rounds and eight).
 bool large_tiles(int64_t p, int64_t q, int64_t batches)
 {
     const int64_t large = ceil_to(p, 256) * (int64_t)ceil_to(q, 256) * batches;
     const int64_t medium = ceil_to(p, 128) * (int64_t)ceil_to(q, 128) * batches;
-    return ceil_to(large, 256) <= 0.54 * ceil_to(medium, 512);
+    return ceil_to(large, 256) <= 0.58 * ceil_to(medium, 512);
 }
 
-// The tile of a product of p classes and q rows, `batches` of them, of `steps`
-// steps: 16 rows where there are no more (one row of 131072 x 4096: w streams at
-// 6 TB/s). Waves of 64 x 128 results read fewer bytes from the tiles than their
-// transpose (131072 x 8192 x 4096: 6.52 against 6.78 ms), but reduce over the
-// classes four times as often (16384 x 4096 x 256: 785 against 697 us).
-Kind choose(int64_t p, int64_t q, int64_t batches, int64_t steps)
+// The tile of a product of p classes and q rows, `batches` of them: 16 rows where
+// there are no more (one row of 131072 x 4096: w streams at 6 TB/s).
+Kind choose(int64_t p, int64_t q, int64_t batches)
 {
     if (q <= 16)
         return Kind::narrow;
-    if (!large_tiles(p, q, batches))
-        return Kind::medium;
-    return steps >= 32 ? Kind::tall : Kind::large;
+    return large_tiles(p, q, batches) ? Kind::large : Kind::medium;
 }
 // The same for the gradients, whose p axis is the features: no more than 64 of
 // them would leave half of a 128 wide tile empty.
@@ -1083,12 +1139,11 @@ Kind choose_grad(int64_t dim, int64_t q, int64_t batches, bool narrow)
         return Kind::narrow;
     if (dim <= 64)
         return Kind::thin;
-    return large_tiles(dim, q, batches) ? Kind::tall : Kind::medium;
+    return large_tiles(dim, q, batches) ? Kind::large : Kind::medium;
 }
-bool is_large(Kind k) { return k == Kind::large || k == Kind::tall; }
-int tile_p(Kind k) { return is_large(k) ? 256 : k == Kind::thin ? 64 : 128; }
-int tile_q(Kind k) { return is_large(k) ? 256 : k == Kind::narrow ? 16 : 128; }
-int waves_p(Kind k) { return k == Kind::narrow ? Narrow::WP : k == Kind::tall ? Tall::WP : 2; }
+int tile_p(Kind k) { return k == Kind::large ? 256 : k == Kind::thin ? 64 : 128; }
+int tile_q(Kind k) { return k == Kind::large ? 256 : k == Kind::narrow ? 16 : 128; }
+int waves_p(Kind k) { return k == Kind::narrow ? Narrow::WP : 2; }
 
 template <class ELEM, bool PLANES, bool PK, bool QK, class S, class F>
 void launch_shape(Product a, int64_t cover_p, int64_t cover_q, const F &f, hipStream_t s)
@@ -1105,14 +1160,11 @@ void launch_shape(Product a, int64_t cover_p, int64_t cover_q, const F &f, hipSt
 template <class ELEM, bool PLANES, bool PK, bool QK, class F>
 void launch_product(Kind kind, const Product &a, int64_t cover_p, int64_t cover_q, const F &f, hipStream_t s)
 {
-    if (kind == Kind::tall)
-        launch_shape<ELEM, PLANES, PK, QK, Tall>(a, cover_p, cover_q, f, s);
+    if (kind == Kind::large)
+        launch_shape<ELEM, PLANES, PK, QK, std::conditional_t<PK, Tall, Large>>(a, cover_p, cover_q, f, s);
     else if (kind == Kind::medium)
         launch_shape<ELEM, PLANES, PK, QK, Medium>(a, cover_p, cover_q, f, s);
-    else if (kind == Kind::large) {
-        if constexpr (!PK)
-            launch_shape<ELEM, PLANES, PK, QK, Large>(a, cover_p, cover_q, f, s);
-    } else if (kind == Kind::thin) {
+    else if (kind == Kind::thin) {
         if constexpr (PK)
             launch_shape<ELEM, PLANES, PK, QK, Thin>(a, cover_p, cover_q, f, s);
     } else if constexpr (!QK)
@@ -1131,7 +1183,6 @@ struct Offsets {
 
 bool aligned16(const void *p) { return ((uintptr_t)p & 15) == 0; }
 int planes(const CeProblem &p) { return p.type == ElemType::f32 ? 3 : 1; }
-int dim_steps(const CeProblem &p) { return ceil_to(p.dim, kCeStep) * (planes(p) == 3 ? kPlaneProducts : 1); }
 int64_t all_rows(const CeProblem &p) { return (int64_t)p.samples * p.rows; }
 
 // x is copied where its rows are no whole steps (the copy's zeros are what ends
@@ -1211,7 +1262,7 @@ CeForwardPlan ce_plan_forward(const CeProblem &p)
     CeForwardPlan f{};
     choose_packs(p, &f.pack_x, &f.pack_w);
     f.dim_pad = (int)pad_to(p.dim, kCeStep);
-    const Kind kind = choose(p.classes, p.rows, p.samples, dim_steps(p));
+    const Kind kind = choose(p.classes, p.rows, p.samples);
     f.parts = ceil_to(p.classes, tile_p(kind)) * waves_p(kind);
     const int64_t n = all_rows(p);
     Offsets o;
@@ -1252,7 +1303,7 @@ void ce_forward(const CeProblem &p, const CeForwardPlan &plan, uint8_t *ws, floa
         a.steps = plan.dim_pad / kCeStep;
         a.samples = p.samples;
         a.splits = 1;
-        launch_product<ELEM, decltype(cut)::value, false, false>(choose(p.classes, p.rows, p.samples, dim_steps(p)), a,
+        launch_product<ELEM, decltype(cut)::value, false, false>(choose(p.classes, p.rows, p.samples), a,
                                                                  p.classes, p.rows,
                                                                  FinishStats{target, part, picked, ticket, scale2_of(p)}, s);
     });
@@ -1378,7 +1429,7 @@ void ce_backward(const CeProblem &p, const CeBackwardPlan &plan, uint8_t *ws, co
                     a.splits = 1;
                     const int64_t r0 = (int64_t)s0 * p.rows;
                     launch_product<ELEM, PLANES, false, false>(
-                        choose(nc, p.rows, ns, dim_steps(p)), a, nc_pad, plan.rows_pad,
+                        choose(nc, p.rows, ns), a, nc_pad, plan.rows_pad,
                         FinishGrad<PLANES>{target, coef, r0, g, plane_g, scale2_of(p), plan.rows_pad, plan.ld_g, c0}, s);
                 }
                 Operand G;
