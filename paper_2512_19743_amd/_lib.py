@@ -406,18 +406,20 @@ def _on_gpu(name: str, t: torch.Tensor, types, like: Optional[torch.Tensor] = No
     return t
 
 
-def _ptr(t: Optional[torch.Tensor]):
-    return ctypes.c_void_p(t.data_ptr()) if t is not None else None
+def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
+    return t.data_ptr() if t is not None else None
 
 
 class _Queued:
     """The device and stream of a call: what is allocated within belongs to that stream."""
 
+    __slots__ = ("guard", "device", "stream")
+
     def __init__(self, device: torch.device, stream: Optional[torch.cuda.Stream]):
-        if stream is not None and stream.device != device:
-            raise ValueError(f"stream must be on {device}, got {stream.device}")
         self.guard = None
         if stream is not None:
+            if stream.device != device:
+                raise ValueError(f"stream must be on {device}, got {stream.device}")
             self.guard = torch.cuda.stream(stream)
         elif torch.cuda.current_device() != device.index:
             self.guard = torch.cuda.device(device)
@@ -432,6 +434,32 @@ class _Queued:
         if self.guard is not None:
             self.guard.__exit__(*exc)
         return False
+
+
+# Workspace sizes follow from the sizes and the pointers' alignment alone.
+_workspace_sizes: dict = {}
+
+
+def _workspace(key, device, query) -> torch.Tensor:
+    n = _workspace_sizes.get(key)
+    if n is None:
+        need = ctypes.c_size_t()
+        query(ctypes.byref(need))
+        if len(_workspace_sizes) >= 4096:
+            _workspace_sizes.clear()
+        n = _workspace_sizes[key] = need.value
+    return torch.empty(n, dtype=torch.uint8, device=device)
+
+
+def _ce_workspace(d, x, w, backward: bool) -> torch.Tensor:
+    key = (backward, d.dtype, d.samples, d.rows, d.classes, d.dim, d.reduction, d.z_weight != 0.0, x.data_ptr() & 15,
+           w.data_ptr() & 15)
+
+    def query(n):
+        _check("apml_linear_ce_workspace", load().apml_linear_ce_workspace(
+            ctypes.byref(d), _ptr(x), _ptr(w), None if backward else n, n if backward else None))
+
+    return _workspace(key, x.device, query)
 
 
 def _linear_ce_desc(x, w, target, scale, z_weight, ignore_index, reduction) -> apml_linear_ce_desc:
@@ -476,12 +504,9 @@ def apml_linear_ce_forward(x: torch.Tensor, w: torch.Tensor, target: torch.Tenso
         loss = torch.empty(target.shape if reduction == "none" else (), dtype=torch.float32, device=x.device)
         if keep_state:
             state = torch.empty(d.samples * d.rows + 1, 4, dtype=torch.float32, device=x.device)
-        need = ctypes.c_size_t()
-        _check("apml_linear_ce_workspace",
-               load().apml_linear_ce_workspace(ctypes.byref(d), _ptr(x), _ptr(w), ctypes.byref(need), None))
-        ws = torch.empty(need.value, dtype=torch.uint8, device=x.device)
+        ws = _ce_workspace(d, x, w, False)
         st = load().apml_linear_ce_forward(ctypes.byref(d), _ptr(x), _ptr(w), _ptr(target), _ptr(loss), _ptr(state),
-                                           _ptr(ws), need.value, queue)
+                                           _ptr(ws), ws.numel(), queue)
     _check("apml_linear_ce_forward", st)
     return loss, state
 
@@ -507,12 +532,9 @@ def apml_linear_ce_backward(state: torch.Tensor, x: torch.Tensor, w: torch.Tenso
         gw = make(w) if want_grad_w else None
         if d.rows == 0:
             return gx, gw
-        need = ctypes.c_size_t()
-        _check("apml_linear_ce_workspace",
-               load().apml_linear_ce_workspace(ctypes.byref(d), _ptr(x), _ptr(w), None, ctypes.byref(need)))
-        ws = torch.empty(need.value, dtype=torch.uint8, device=x.device)
+        ws = _ce_workspace(d, x, w, True)
         st = load().apml_linear_ce_backward(ctypes.byref(d), _ptr(x), _ptr(w), _ptr(target), _ptr(state),
-                                            _ptr(grad_loss), _ptr(gx), _ptr(gw), _ptr(ws), need.value, queue)
+                                            _ptr(grad_loss), _ptr(gx), _ptr(gw), _ptr(ws), ws.numel(), queue)
     _check("apml_linear_ce_backward", st)
     return gx, gw
 
@@ -579,11 +601,10 @@ def apml_balance_forward(logits: torch.Tensor, experts: Optional[torch.Tensor] =
         if counts is None:
             counts = torch.empty(shape, dtype=torch.int64, device=logits.device)
         state = torch.empty(d.samples, d.experts + 1, dtype=torch.float32, device=logits.device) if keep_state else None
-        need = ctypes.c_size_t()
-        _check("apml_balance_workspace", load().apml_balance_workspace(ctypes.byref(d), ctypes.byref(need)))
-        ws = torch.empty(need.value, dtype=torch.uint8, device=logits.device)
+        ws = _workspace(("balance", d.dtype, d.samples, d.tokens, d.experts), logits.device, lambda n: _check(
+            "apml_balance_workspace", load().apml_balance_workspace(ctypes.byref(d), n)))
         st = load().apml_balance_forward(ctypes.byref(d), _ptr(logits), _ptr(experts), _ptr(valid), _ptr(counts),
-                                         _ptr(loss), _ptr(state), _ptr(ws), need.value, queue)
+                                         _ptr(loss), _ptr(state), _ptr(ws), ws.numel(), queue)
     _check("apml_balance_forward", st)
     return loss, counts, state
 

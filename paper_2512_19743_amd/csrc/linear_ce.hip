@@ -758,6 +758,11 @@ struct FinishPart {
 template <class IN> __device__ __forceinline__ float get(const void *in, int64_t at) { return IN::to(((const uint16_t *)in)[at]); }
 template <> __device__ __forceinline__ float get<float>(const void *in, int64_t at) { return ((const float *)in)[at]; }
 
+// Eight neighbours at any element.
+template <class T> struct __attribute__((packed, aligned(sizeof(T)))) Loose {
+    T v[8];
+};
+
 struct PackJob {
     const void *in;
     uint16_t *out;
@@ -798,19 +803,20 @@ template <class IN> __global__ __launch_bounds__(kBlock) void k_ce_pack(PackJobs
     float v[8];
     const int64_t at = row * jobs.dim + d;
     constexpr int size = std::is_same_v<IN, float> ? 4 : 2;
-    if (keep && d + 8 <= jobs.dim && (((uintptr_t)p.in + at * size) & 15) == 0) {
+    if (keep && d + 8 <= jobs.dim) {
+        // eight neighbours wherever they lie: a global load of 16 bytes needs no
+        // more alignment than its elements (50001 x 1003 half precision: 2.5 TB/s
+        // element by element)
         if constexpr (size == 4) {
-            const f32x4 lo = ((const f32x4 *)((const float *)p.in + at))[0], hi = ((const f32x4 *)((const float *)p.in + at))[1];
-#pragma unroll
-            for (int u = 0; u < 4; ++u) {
-                v[u] = lo[u] * f;
-                v[u + 4] = hi[u] * f;
-            }
-        } else {
-            const i16x8 raw = *(const i16x8 *)((const uint16_t *)p.in + at);
+            const Loose<float> raw = *(const Loose<float> *)((const float *)p.in + at);
 #pragma unroll
             for (int u = 0; u < 8; ++u)
-                v[u] = IN::to((uint16_t)raw[u]) * f;
+                v[u] = raw.v[u] * f;
+        } else {
+            const Loose<uint16_t> raw = *(const Loose<uint16_t> *)((const uint16_t *)p.in + at);
+#pragma unroll
+            for (int u = 0; u < 8; ++u)
+                v[u] = IN::to(raw.v[u]) * f;
         }
     } else {
 #pragma unroll
@@ -859,7 +865,7 @@ __global__ __launch_bounds__(kBlock) void k_ce_rows(const float2 *part, int part
     const int64_t row = (int64_t)blockIdx.x * ROWS + r;
     float m = -kInf, sum = 0.0f;
     if (row < n) {
-        constexpr int U = 8; // loads in flight
+        constexpr int U = THREADS == 4 ? 16 : 8; // loads in flight
         for (int k = k0; k < parts; k += THREADS * U) {
             float2 v[U];
 #pragma unroll
@@ -881,6 +887,7 @@ __global__ __launch_bounds__(kBlock) void k_ce_rows(const float2 *part, int part
     }
     sm[k0][r] = make_float2(m, sum);
     __syncthreads();
+    constexpr int LEFT = THREADS < 16 ? THREADS : 16;
     if constexpr (THREADS > 16) { // 16 are left, each with a fixed share
         if (k0 < 16) {
             float top = m;
@@ -900,11 +907,11 @@ __global__ __launch_bounds__(kBlock) void k_ce_rows(const float2 *part, int part
             const int t = target[row];
             const float z = t >= 0 ? picked[row] : -kInf;
             float top = z;
-            for (int k = 0; k < 16; ++k)
+            for (int k = 0; k < LEFT; ++k)
                 top = fmaxf(top, sm[k][r].x);
             const float base = top == -kInf ? 0.0f : top;
             double others = 0.0;
-            for (int k = 0; k < 16; ++k)
+            for (int k = 0; k < LEFT; ++k)
                 others += (double)sm[k][r].y * (double)exp2f(sm[k][r].x - base);
             const double mine = t >= 0 ? (double)exp2f(z - base) : 0.0;
             const double all = others + mine;
@@ -930,6 +937,7 @@ __global__ __launch_bounds__(kBlock) void k_ce_rows(const float2 *part, int part
     __syncthreads();
     if (threadIdx.x == 0) {
         LossSum s = sl[0];
+#pragma unroll 8
         for (int k = 1; k < ROWS; ++k) {
             s.sum += sl[k].sum;
             s.count += sl[k].count;
@@ -1116,11 +1124,12 @@ enum class Kind { large, medium, narrow, thin };
 // Whether 256 x 256 tiles, one a compute unit, end before 128 x 128 ones, two a
 // compute unit: rounds of each, a round of the latter taking 0.58 of the former's
 // time (8192 x 8192 x 1024: 116 us against 134 in four rounds and eight).
+constexpr double kMediumRound = 0.58;
 bool large_tiles(int64_t p, int64_t q, int64_t batches)
 {
     const int64_t large = ceil_to(p, 256) * (int64_t)ceil_to(q, 256) * batches;
     const int64_t medium = ceil_to(p, 128) * (int64_t)ceil_to(q, 128) * batches;
-    return ceil_to(large, 256) <= 0.58 * ceil_to(medium, 512);
+    return ceil_to(large, 256) <= kMediumRound * ceil_to(medium, 512);
 }
 
 // The tile of a product of p classes and q rows, `batches` of them: 16 rows where
@@ -1131,18 +1140,49 @@ Kind choose(int64_t p, int64_t q, int64_t batches)
         return Kind::narrow;
     return large_tiles(p, q, batches) ? Kind::large : Kind::medium;
 }
-// The same for the gradients, whose p axis is the features: no more than 64 of
-// them would leave half of a 128 wide tile empty.
-Kind choose_grad(int64_t dim, int64_t q, int64_t batches, bool narrow)
+// The same for the gradients, whose p axis is the features and whose sums, over
+// `steps` steps, may be cut into parts: no more than 64 features would leave half
+// of a 128 wide tile empty; else the tile and the parts that end first, in steps
+// of the large tile: rounds, and each part's results written and read again in
+// float32 (at about 4 TB/s, 6 MB a step).
+struct Cut {
+    Kind kind;
+    int splits;
+};
+Cut choose_grad(int64_t dim, int64_t q, int64_t batches, int64_t steps, int planes, bool narrow)
 {
-    if (narrow && q <= 16)
-        return Kind::narrow;
-    if (dim <= 64)
-        return Kind::thin;
-    return large_tiles(dim, q, batches) ? Kind::large : Kind::medium;
+    const int64_t least = planes > 1 ? 2 : 8; // a float32 step is six
+    const auto parts = [&](int64_t tiles, int64_t slots) {
+        return std::max<int64_t>(1, std::min<int64_t>({slots / std::max<int64_t>(tiles, 1), steps / least, 64}));
+    };
+    if (dim <= 64 || (narrow && q <= 16)) {
+        const Kind kind = narrow && q <= 16 ? Kind::narrow : Kind::thin;
+        const int64_t tiles = ceil_to(dim, kind == Kind::thin ? 64 : 128) *
+                              (int64_t)ceil_to(q, kind == Kind::thin ? 128 : 16) * batches;
+        return {kind, tiles >= 256 ? 1 : (int)parts(tiles, 512)};
+    }
+    const int64_t large = ceil_to(dim, 256) * (int64_t)ceil_to(q, 256) * batches;
+    const int64_t medium = ceil_to(dim, 128) * (int64_t)ceil_to(q, 128) * batches;
+    const double work = (double)steps * (planes > 1 ? kPlaneProducts : 1);
+    const auto cost = [&](int64_t tiles, int64_t slots, int64_t cut, double round) {
+        const double join = cut > 1 ? (double)(cut + 1) * dim * q * batches * 8.0 / 6e6 + 4.0 : 0.0;
+        return (double)ceil_to(tiles * cut, slots) * ((work + cut - 1) / cut + 4.0) * round + join;
+    };
+    Cut best{Kind::medium, 1};
+    double least_cost = cost(medium, 512, 1, kMediumRound);
+    const auto consider = [&](Kind kind, int64_t tiles, int64_t slots, double round) {
+        const int64_t most = std::min<int64_t>(parts(tiles, 1 << 20), std::max<int64_t>(1, 2 * slots / tiles));
+        for (int64_t cut = 1; cut <= most; ++cut)
+            if (const double c = cost(tiles, slots, cut, round); c < least_cost) {
+                least_cost = c;
+                best = {kind, (int)cut};
+            }
+    };
+    consider(Kind::medium, medium, 512, kMediumRound);
+    consider(Kind::large, large, 256, 1.0);
+    return best;
 }
 int tile_p(Kind k) { return k == Kind::large ? 256 : k == Kind::thin ? 64 : 128; }
-int tile_q(Kind k) { return k == Kind::large ? 256 : k == Kind::narrow ? 16 : 128; }
 int waves_p(Kind k) { return k == Kind::narrow ? Narrow::WP : 2; }
 
 template <class ELEM, bool PLANES, bool PK, bool QK, class S, class F>
@@ -1254,8 +1294,9 @@ template <class F> void by_type(ElemType t, F f)
 
 // Threads of k_ce_rows a row: with few rows, as many as it takes to have the
 // parts' loads in flight together (one row of 131072 classes, 4096 parts: 16
-// threads 105 us, 256 threads 5.5 us).
-static int row_threads(int64_t n) { return n >= 256 ? 16 : kBlock; }
+// threads 105 us, 256 threads 5.5 us), with many as few as let a workgroup read
+// whole lines of each part.
+static int row_threads(int64_t n) { return n >= 32768 ? 4 : n >= 256 ? 16 : kBlock; }
 
 CeForwardPlan ce_plan_forward(const CeProblem &p)
 {
@@ -1307,12 +1348,17 @@ void ce_forward(const CeProblem &p, const CeForwardPlan &plan, uint8_t *ws, floa
                                                                  p.classes, p.rows,
                                                                  FinishStats{target, part, picked, ticket, scale2_of(p)}, s);
     });
-    if (row_threads(n) == 16)
-        k_ce_rows<16><<<dim3(blocks_for(n, kBlock / 16)), dim3(kBlock), 0, s>>>(
+    const auto join = [&](auto threads) {
+        constexpr int T = decltype(threads)::value;
+        k_ce_rows<T><<<dim3(blocks_for(n, kBlock / T)), dim3(kBlock), 0, s>>>(
             part, plan.parts, picked, target, n, p.z_weight, p.reduction, loss, rows, sums, ticket, loss, total);
+    };
+    if (row_threads(n) == 4)
+        join(std::integral_constant<int, 4>{});
+    else if (row_threads(n) == 16)
+        join(std::integral_constant<int, 16>{});
     else
-        k_ce_rows<kBlock><<<dim3(blocks_for(n, 1)), dim3(kBlock), 0, s>>>(
-            part, plan.parts, picked, target, n, p.z_weight, p.reduction, loss, rows, sums, ticket, loss, total);
+        join(std::integral_constant<int, kBlock>{});
 }
 
 namespace {
@@ -1324,13 +1370,14 @@ namespace {
 // float32 1.37, 1.20, 1.12, 1.33 ms).
 constexpr int64_t kPieceBytes = (int64_t)256 << 20;
 
-// Parts of a sum of `steps` steps so that a product of few tiles fills the card,
-// each of at least `least` steps: a part's results are written and read again.
-int choose_splits(int64_t tiles, int64_t steps, int least)
+// The products for grad_x and grad_w of a whole piece.
+Cut cut_x(const CeProblem &p, const CeBackwardPlan &b)
 {
-    if (tiles >= 256)
-        return 1;
-    return (int)std::max<int64_t>(1, std::min<int64_t>({512 / std::max<int64_t>(tiles, 1), steps / least, 64}));
+    return choose_grad(p.dim, p.rows, b.piece_samples, b.ld_g / kCeStep, planes(p), true);
+}
+Cut cut_w(const CeProblem &p, const CeBackwardPlan &b)
+{
+    return choose_grad(p.dim, b.piece_classes, b.piece_samples, b.rows_pad / kCeStep, planes(p), false);
 }
 
 } // namespace
@@ -1353,12 +1400,8 @@ CeBackwardPlan ce_plan_backward(const CeProblem &p, bool want_x, bool want_w)
         b.piece_classes = (int)std::min<int64_t>(p.classes, pad_to(ceil_to(p.classes, pieces), 256));
     }
     b.ld_g = (int)pad_to(b.piece_classes, kCeStep);
-    const int least = p.type == ElemType::f32 ? 2 : 8; // a float32 step is six
-    const Kind kx = choose_grad(p.dim, p.rows, b.piece_samples, true), kw = choose_grad(p.dim, b.piece_classes, b.piece_samples, false);
-    b.split_x = choose_splits((int64_t)ceil_to(p.dim, tile_p(kx)) * ceil_to(p.rows, tile_q(kx)) * b.piece_samples,
-                              b.ld_g / kCeStep, least);
-    b.split_w = choose_splits((int64_t)ceil_to(p.dim, tile_p(kw)) * ceil_to(b.piece_classes, tile_q(kw)) * b.piece_samples,
-                              b.rows_pad / kCeStep, least);
+    b.split_x = cut_x(p, b).splits;
+    b.split_w = cut_w(p, b).splits;
     b.sum_x = b.split_x > 1 || b.piece_classes < p.classes;
     const int64_t ld = pad_to(p.dim, 4);
     Offsets o;
@@ -1448,7 +1491,7 @@ void ce_backward(const CeProblem &p, const CeBackwardPlan &plan, uint8_t *ws, co
                     a.q.k = nc_pad;
                     a.steps = nc_pad / kCeStep;
                     a.samples = ns;
-                    const Kind kind = choose_grad(p.dim, p.rows, plan.piece_samples, true);
+                    const Kind kind = cut_x(p, plan).kind;
                     if (plan.sum_x) {
                         a.splits = plan.split_x;
                         const int64_t sample = (int64_t)p.rows * ld, split = plan.piece_samples * sample;
@@ -1478,7 +1521,7 @@ void ce_backward(const CeProblem &p, const CeBackwardPlan &plan, uint8_t *ws, co
                     a.steps = plan.rows_pad / kCeStep;
                     a.samples = ns;
                     a.splits = plan.split_w;
-                    const Kind kind = choose_grad(p.dim, plan.piece_classes, plan.piece_samples, false);
+                    const Kind kind = cut_w(p, plan).kind;
                     const int64_t sample = (int64_t)p.classes * p.dim;
                     void *to = (uint8_t *)grad_w + (s0 * sample + (int64_t)c0 * p.dim) * elem_size(p.type);
                     if (plan.split_w > 1) {
