@@ -217,14 +217,16 @@ __device__ __forceinline__ i16x8 fragment(const lds_char *tile, int r0, int i, i
 
 // The tile shapes. A workgroup takes TP x TQ results, its waves WP x WQ of them,
 // with BUFS steps' tiles in shared memory. WOVEN: the fragments of the next half
-// step are read between the matrix instructions of this one.
-template <int TP_, int TQ_, int WP_, int WQ_, int BUFS_, bool WOVEN_ = false> struct Shape {
+// step are read between the matrix instructions of this one. TRIPLE, for float32:
+// a step's tile holds all three planes of both operands and gives all six
+// products, half of the loads that six steps of one plane each need.
+template <int TP_, int TQ_, int WP_, int WQ_, int BUFS_, bool WOVEN_ = false, bool TRIPLE_ = false> struct Shape {
     static constexpr int TP = TP_, TQ = TQ_, WP = WP_, WQ = WQ_, BUFS = BUFS_;
-    static constexpr bool WOVEN = WOVEN_;
+    static constexpr bool WOVEN = WOVEN_, TRIPLE = TRIPLE_;
     static_assert(!WOVEN || BUFS == 2, "two tiles in turn");
     static constexpr int waves = WP * WQ, threads = 64 * waves;
     static constexpr int SP = TP / WP / 16, SQ = TQ / WQ / 16; // 16 x 16 results of a wave
-    static constexpr int stage = (TP + TQ) * 128;
+    static constexpr int stage = (TP + TQ) * 128 * (TRIPLE ? 3 : 1);
     static constexpr int lds = stage * BUFS;
     static constexpr int LP = TP / 8 / waves;                                    // loads of a wave for P
     static constexpr int LQ = (TQ / 8 + waves - 1) / waves;                      // and for Q
@@ -269,7 +271,7 @@ __global__ __launch_bounds__(S::threads) void k_product(Product a, Finish finish
     // steps of this part of the sum
     const int first = (int)((int64_t)a.steps * at.split / a.splits);
     const int last = (int)((int64_t)a.steps * (at.split + 1) / a.splits);
-    const int n = last - first, total = PLANES ? n * kPlaneProducts : n;
+    const int n = last - first, total = PLANES && !S::TRIPLE ? n * kPlaneProducts : n;
 
     uint32_t op[S::LP], oq[S::LQ];
     const auto offsets = [&](int step) {
@@ -289,7 +291,7 @@ __global__ __launch_bounds__(S::threads) void k_product(Product a, Finish finish
     offsets(0);
     const auto load = [&](int i) {
         int step = first + i, pp = 0, pq = 0;
-        if constexpr (PLANES) {
+        if constexpr (PLANES && !S::TRIPLE) {
             const int prod = i / n;
             step = first + i - prod * n;
             pp = (0x120100 >> (4 * prod)) & 15; // planes 0 0 1 0 2 1
@@ -297,15 +299,19 @@ __global__ __launch_bounds__(S::threads) void k_product(Product a, Finish finish
         }
         if (ragged >= 0 && (step == ragged || step == first))
             offsets(step);
-        const i32x4 rp = buffer_at(base_p + 2 * (uint64_t)(step * step_p + pp * a.p.plane));
-        const i32x4 rq = buffer_at(base_q + 2 * (uint64_t)(step * step_q + pq * a.q.plane));
-        const uint32_t to = lds0 + (i % S::BUFS) * S::stage;
+        uint32_t to = lds0 + (i % S::BUFS) * S::stage;
 #pragma unroll
-        for (int j = 0; j < S::LP; ++j)
-            load_to_lds(rp, op[j], to + (wave * S::LP + j) * 1024);
+        for (int plane = 0; plane < (S::TRIPLE ? 3 : 1); ++plane) {
+            const i32x4 rp = buffer_at(base_p + 2 * (uint64_t)(step * step_p + (pp + plane) * a.p.plane));
+            const i32x4 rq = buffer_at(base_q + 2 * (uint64_t)(step * step_q + (pq + plane) * a.q.plane));
 #pragma unroll
-        for (int j = 0; j < S::LQ; ++j)
-            load_to_lds(rq, oq[j], to + S::TP * 128 + ((wave * S::LQ + j) % (S::TQ / 8)) * 1024);
+            for (int j = 0; j < S::LP; ++j)
+                load_to_lds(rp, op[j], to + (wave * S::LP + j) * 1024);
+#pragma unroll
+            for (int j = 0; j < S::LQ; ++j)
+                load_to_lds(rq, oq[j], to + S::TP * 128 + ((wave * S::LQ + j) % (S::TQ / 8)) * 1024);
+            to += (S::TP + S::TQ) * 128;
+        }
     };
 
     // what the finish needs of its rows is on its way during the products
@@ -319,8 +325,9 @@ __global__ __launch_bounds__(S::threads) void k_product(Product a, Finish finish
         for (int j = 0; j < S::SQ; ++j)
             acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 
-    const auto read = [&](int i, int h, i16x8 (&fp)[S::SP], i16x8 (&fq)[S::SQ]) {
-        const lds_char *tp = (const lds_char *)smem + (i % S::BUFS) * S::stage, *tq = tp + S::TP * 128;
+    const auto read = [&](int i, int h, i16x8 (&fp)[S::SP], i16x8 (&fq)[S::SQ], int plane = 0) {
+        const lds_char *tp = (const lds_char *)smem + (i % S::BUFS) * S::stage + plane * ((S::TP + S::TQ) * 128);
+        const lds_char *tq = tp + S::TP * 128;
 #pragma unroll
         for (int j = 0; j < S::SQ; ++j)
             fq[j] = fragment<S::TQ, QK, false>(tq, at.wq * (S::SQ * 16), j, h, lane);
@@ -398,9 +405,22 @@ __global__ __launch_bounds__(S::threads) void k_product(Product a, Finish finish
                 load(i + S::BUFS - 1);
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                i16x8 fp[S::SP], fq[S::SQ];
-                read(i, h, fp, fq);
-                multiply(fp, fq);
+                if constexpr (S::TRIPLE) {
+                    i16x8 fp[3][S::SP], fq[3][S::SQ];
+#pragma unroll
+                    for (int plane = 0; plane < 3; ++plane)
+                        read(i, h, fp[plane], fq[plane], plane);
+                    multiply(fp[0], fq[0]);
+                    multiply(fp[0], fq[1]);
+                    multiply(fp[1], fq[0]);
+                    multiply(fp[1], fq[1]);
+                    multiply(fp[0], fq[2]);
+                    multiply(fp[2], fq[0]);
+                } else {
+                    i16x8 fp[S::SP], fq[S::SQ];
+                    read(i, h, fp, fq);
+                    multiply(fp, fq);
+                }
             }
         }
     }
@@ -1115,6 +1135,7 @@ using Tall = Shape<256, 256, 4, 2, 2, true>;  // the gradients' (8192 x 4096 x 8
 using Medium = Shape<128, 128, 2, 2, 2>;
 using Narrow = Shape<128, 16, 4, 1, 4>;
 using Thin = Shape<64, 128, 2, 2, 2>;
+using ThinTriple = Shape<64, 128, 2, 4, 2, false, true>; // 10 of 64 x 2048 x 2048: 53 us; one plane a step 68
 
 int ceil_to(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
 int64_t pad_to(int64_t a, int64_t b) { return (a + b - 1) / b * b; }
@@ -1152,34 +1173,30 @@ struct Cut {
 Cut choose_grad(int64_t dim, int64_t q, int64_t batches, int64_t steps, int planes, bool narrow)
 {
     const int64_t least = planes > 1 ? 2 : 8; // a float32 step is six
-    const auto parts = [&](int64_t tiles, int64_t slots) {
-        return std::max<int64_t>(1, std::min<int64_t>({slots / std::max<int64_t>(tiles, 1), steps / least, 64}));
-    };
-    if (dim <= 64 || (narrow && q <= 16)) {
-        const Kind kind = narrow && q <= 16 ? Kind::narrow : Kind::thin;
-        const int64_t tiles = ceil_to(dim, kind == Kind::thin ? 64 : 128) *
-                              (int64_t)ceil_to(q, kind == Kind::thin ? 128 : 16) * batches;
-        return {kind, tiles >= 256 ? 1 : (int)parts(tiles, 512)};
-    }
-    const int64_t large = ceil_to(dim, 256) * (int64_t)ceil_to(q, 256) * batches;
-    const int64_t medium = ceil_to(dim, 128) * (int64_t)ceil_to(q, 128) * batches;
     const double work = (double)steps * (planes > 1 ? kPlaneProducts : 1);
-    const auto cost = [&](int64_t tiles, int64_t slots, int64_t cut, double round) {
-        const double join = cut > 1 ? (double)(cut + 1) * dim * q * batches * 8.0 / 6e6 + 4.0 : 0.0;
-        return (double)ceil_to(tiles * cut, slots) * ((work + cut - 1) / cut + 4.0) * round + join;
-    };
     Cut best{Kind::medium, 1};
-    double least_cost = cost(medium, 512, 1, kMediumRound);
-    const auto consider = [&](Kind kind, int64_t tiles, int64_t slots, double round) {
-        const int64_t most = std::min<int64_t>(parts(tiles, 1 << 20), std::max<int64_t>(1, 2 * slots / tiles));
-        for (int64_t cut = 1; cut <= most; ++cut)
-            if (const double c = cost(tiles, slots, cut, round); c < least_cost) {
+    double least_cost = HUGE_VAL;
+    // slots: workgroups that run at once; round: their step's time
+    const auto consider = [&](Kind kind, int tile_p, int tile_q, int64_t slots, double round) {
+        const int64_t tiles = ceil_to(dim, tile_p) * (int64_t)ceil_to(q, tile_q) * batches;
+        const int64_t most = std::max<int64_t>(1, std::min<int64_t>({2 * slots / tiles, steps / least, 64}));
+        for (int64_t cut = 1; cut <= most; ++cut) {
+            const double join = cut > 1 ? (double)(cut + 1) * dim * q * batches * 8.0 / 6e6 + 4.0 : 0.0;
+            const double c = (double)ceil_to(tiles * cut, slots) * ((work + cut - 1) / cut + 4.0) * round + join;
+            if (c < least_cost) {
                 least_cost = c;
                 best = {kind, (int)cut};
             }
+        }
     };
-    consider(Kind::medium, medium, 512, kMediumRound);
-    consider(Kind::large, large, 256, 1.0);
+    if (narrow && q <= 16)
+        consider(Kind::narrow, 128, 16, 512, 0.2);
+    else if (dim <= 64)
+        consider(Kind::thin, 64, 128, planes > 1 ? 256 : 768, planes > 1 ? 0.24 : 0.5);
+    else {
+        consider(Kind::medium, 128, 128, 512, kMediumRound);
+        consider(Kind::large, 256, 256, 256, 1.0);
+    }
     return best;
 }
 int tile_p(Kind k) { return k == Kind::large ? 256 : k == Kind::thin ? 64 : 128; }
@@ -1206,7 +1223,7 @@ void launch_product(Kind kind, const Product &a, int64_t cover_p, int64_t cover_
         launch_shape<ELEM, PLANES, PK, QK, Medium>(a, cover_p, cover_q, f, s);
     else if (kind == Kind::thin) {
         if constexpr (PK)
-            launch_shape<ELEM, PLANES, PK, QK, Thin>(a, cover_p, cover_q, f, s);
+            launch_shape<ELEM, PLANES, PK, QK, std::conditional_t<PLANES, ThinTriple, Thin>>(a, cover_p, cover_q, f, s);
     } else if constexpr (!QK)
         launch_shape<ELEM, PLANES, PK, QK, Narrow>(a, cover_p, cover_q, f, s);
 }

@@ -180,6 +180,23 @@ def test_the_same_bits_every_time():
         assert all(torch.equal(a, b) for a, b in zip(r, runs[0]))
 
 
+def test_two_streams_at_once():
+    data = [make(2, 6000 + 50 * k, 60, 3, BF16, seed=k, padded=0.2) for k in range(2)]
+    want = [apml.apml_balance_forward(a, b, valid=c, z_weight=0.1)[:2] for a, b, c in data]
+    streams = [torch.cuda.Stream() for _ in data]
+    for s in streams:
+        s.wait_stream(torch.cuda.current_stream())
+    got = [[], []]
+    for _ in range(4):
+        for k, s in enumerate(streams):
+            a, b, c = data[k]
+            got[k].append(apml.apml_balance_forward(a, b, valid=c, z_weight=0.1, stream=s)[:2])
+    torch.cuda.synchronize()
+    for k in range(2):
+        for r in got[k]:
+            assert torch.equal(r[0], want[k][0]) and torch.equal(r[1], want[k][1])
+
+
 def test_no_tokens():
     for shape in ((0, 8), (3, 0, 8)):
         x = torch.empty(shape, device="cuda", requires_grad=True)

@@ -62,7 +62,8 @@ def test_small_and_odd_sizes(size, dtype):
 
 @pytest.mark.parametrize("dtype", [F32, BF16, F16], ids=["f32", "bf16", "f16"])
 @pytest.mark.parametrize("size", [(0, 4096, 4100, 64), (0, 4160, 17000, 40), (0, 90, 70001, 64), (0, 6000, 300, 1024),
-                                  (4, 2000, 1999, 72), (40, 1024, 1100, 32)], ids=lambda s: "x".join(map(str, s)))
+                                  (4, 2000, 1999, 72), (40, 1024, 1100, 32), (0, 200, 131000, 255), (0, 5000, 700, 515),
+                                  (0, 40000, 260, 96)], ids=lambda s: "x".join(map(str, s)))
 def test_sizes_of_every_tile_piece_and_split(size, dtype):
     # whole tiles of the large shape; several pieces of the classes and of the
     # samples; sums split over classes and over rows
@@ -77,6 +78,12 @@ def test_options(dtype, reduction, z_weight):
     x, w, t = make(0, 100, 333, 96, dtype, ignored=0.3, index=torch.int32)
     g = torch.randn(t.shape if reduction == "none" else (), device="cuda")
     check(x, w, t, reduction=reduction, z_weight=z_weight, scale=-0.8, grad_loss=g)
+
+
+@pytest.mark.parametrize("ignore", [0, 7, 2 ** 40])
+def test_any_class_may_be_the_ignored_one(ignore):
+    x, w, t = make(0, 100, 10, 32, F32)
+    check(x, w, t, ignore_index=ignore, reduction="mean")
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16, F16], ids=["f32", "bf16", "f16"])
@@ -332,6 +339,63 @@ def test_captured_and_replayed():
         torch.cuda.synchronize()
         for _, *got in graphs:
             assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+def test_a_training_steps_gradients_captured():
+    # the public call and its backward pass in one graph, as a captured training step has them
+    x, w, t = make(0, 200, 1500, 96, BF16, ignored=0.1)
+    a, b = x.clone().requires_grad_(True), w.clone().requires_grad_(True)
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(stream):
+        for _ in range(2):
+            torch.autograd.grad(apml.linear_ce_loss(a, b, t), (a, b))
+        stream.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=stream):
+            loss = apml.linear_ce_loss(a, b, t)
+            ga, gb = torch.autograd.grad(loss, (a, b))
+    torch.cuda.synchronize()
+    for k in range(3):
+        y, v, u = make(0, 200, 1500, 96, BF16, ignored=0.1, seed=30 + k)
+        with torch.no_grad():
+            a.copy_(y), b.copy_(v)
+        t.copy_(u)
+        want = check(y, v, u)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(p, q) for p, q in zip((loss.detach(), ga, gb), want))
+
+
+def test_calls_from_two_threads():
+    import threading
+    data = [make(0, 300, 2000 + 100 * k, 128, BF16, seed=k) for k in range(2)]
+    want = [check(*d) for d in data]
+    got, errors = [[], []], []
+
+    def work(k):
+        try:
+            with torch.cuda.stream(torch.cuda.Stream()):
+                for _ in range(4):
+                    a, b = data[k][0].clone().requires_grad_(True), data[k][1].clone().requires_grad_(True)
+                    loss = apml.linear_ce_loss(a, b, data[k][2])
+                    got[k].append((loss.detach(), *torch.autograd.grad(loss, (a, b))))
+                torch.cuda.current_stream().synchronize()
+        except Exception as e:  # noqa: BLE001
+            errors.append(e)
+
+    torch.cuda.synchronize()
+    threads = [threading.Thread(target=work, args=(k,)) for k in range(2)]
+    for th in threads:
+        th.start()
+    for th in threads:
+        th.join()
+    torch.cuda.synchronize()
+    assert not errors, errors
+    for k in range(2):
+        for r in got[k]:
+            assert all(torch.equal(p, q) for p, q in zip(r, want[k]))
 
 
 def test_workspace_of_the_asked_size_and_no_less():
