@@ -1153,11 +1153,12 @@ bool large_tiles(int64_t p, int64_t q, int64_t batches)
     return ceil_to(large, 256) <= kMediumRound * ceil_to(medium, 512);
 }
 
-// The tile of a product of p classes and q rows, `batches` of them: 16 rows where
-// there are no more (one row of 131072 x 4096: w streams at 6 TB/s).
-Kind choose(int64_t p, int64_t q, int64_t batches)
+// The tile of a product of p classes and q rows, `batches` of them. Forward, 16
+// rows where there are no more (one row of 131072 x 4096: w streams at 6 TB/s);
+// backward the logits' gradient is written for whole steps of rows.
+Kind choose(int64_t p, int64_t q, int64_t batches, bool forward)
 {
-    if (q <= 16)
+    if (forward && q <= 16)
         return Kind::narrow;
     return large_tiles(p, q, batches) ? Kind::large : Kind::medium;
 }
@@ -1170,7 +1171,7 @@ struct Cut {
     Kind kind;
     int splits;
 };
-Cut choose_grad(int64_t dim, int64_t q, int64_t batches, int64_t steps, int planes, bool narrow)
+Cut choose_grad(int64_t dim, int64_t q, int64_t batches, int64_t steps, int planes)
 {
     const int64_t least = planes > 1 ? 2 : 8; // a float32 step is six
     const double work = (double)steps * (planes > 1 ? kPlaneProducts : 1);
@@ -1189,11 +1190,9 @@ Cut choose_grad(int64_t dim, int64_t q, int64_t batches, int64_t steps, int plan
             }
         }
     };
-    if (narrow && q <= 16)
-        consider(Kind::narrow, 128, 16, 512, 0.2);
-    else if (dim <= 64)
+    if (dim <= 64) {
         consider(Kind::thin, 64, 128, planes > 1 ? 256 : 768, planes > 1 ? 0.24 : 0.5);
-    else {
+    } else {
         consider(Kind::medium, 128, 128, 512, kMediumRound);
         consider(Kind::large, 256, 256, 256, 1.0);
     }
@@ -1224,7 +1223,7 @@ void launch_product(Kind kind, const Product &a, int64_t cover_p, int64_t cover_
     else if (kind == Kind::thin) {
         if constexpr (PK)
             launch_shape<ELEM, PLANES, PK, QK, std::conditional_t<PLANES, ThinTriple, Thin>>(a, cover_p, cover_q, f, s);
-    } else if constexpr (!QK)
+    } else if constexpr (std::is_same_v<F, FinishStats>)
         launch_shape<ELEM, PLANES, PK, QK, Narrow>(a, cover_p, cover_q, f, s);
 }
 
@@ -1320,7 +1319,7 @@ CeForwardPlan ce_plan_forward(const CeProblem &p)
     CeForwardPlan f{};
     choose_packs(p, &f.pack_x, &f.pack_w);
     f.dim_pad = (int)pad_to(p.dim, kCeStep);
-    const Kind kind = choose(p.classes, p.rows, p.samples);
+    const Kind kind = choose(p.classes, p.rows, p.samples, true);
     f.parts = ceil_to(p.classes, tile_p(kind)) * waves_p(kind);
     const int64_t n = all_rows(p);
     Offsets o;
@@ -1361,7 +1360,7 @@ void ce_forward(const CeProblem &p, const CeForwardPlan &plan, uint8_t *ws, floa
         a.steps = plan.dim_pad / kCeStep;
         a.samples = p.samples;
         a.splits = 1;
-        launch_product<ELEM, decltype(cut)::value, false, false>(choose(p.classes, p.rows, p.samples), a,
+        launch_product<ELEM, decltype(cut)::value, false, false>(choose(p.classes, p.rows, p.samples, true), a,
                                                                  p.classes, p.rows,
                                                                  FinishStats{target, part, picked, ticket, scale2_of(p)}, s);
     });
@@ -1390,11 +1389,11 @@ constexpr int64_t kPieceBytes = (int64_t)256 << 20;
 // The products for grad_x and grad_w of a whole piece.
 Cut cut_x(const CeProblem &p, const CeBackwardPlan &b)
 {
-    return choose_grad(p.dim, p.rows, b.piece_samples, b.ld_g / kCeStep, planes(p), true);
+    return choose_grad(p.dim, p.rows, b.piece_samples, b.ld_g / kCeStep, planes(p));
 }
 Cut cut_w(const CeProblem &p, const CeBackwardPlan &b)
 {
-    return choose_grad(p.dim, b.piece_classes, b.piece_samples, b.rows_pad / kCeStep, planes(p), false);
+    return choose_grad(p.dim, b.piece_classes, b.piece_samples, b.rows_pad / kCeStep, planes(p));
 }
 
 } // namespace
@@ -1489,7 +1488,7 @@ void ce_backward(const CeProblem &p, const CeBackwardPlan &plan, uint8_t *ws, co
                     a.splits = 1;
                     const int64_t r0 = (int64_t)s0 * p.rows;
                     launch_product<ELEM, PLANES, false, false>(
-                        choose(nc, p.rows, ns), a, nc_pad, plan.rows_pad,
+                        choose(nc, p.rows, ns, false), a, nc_pad, plan.rows_pad,
                         FinishGrad<PLANES>{target, coef, r0, g, plane_g, scale2_of(p), plan.rows_pad, plan.ld_g, c0}, s);
                 }
                 Operand G;
