@@ -162,6 +162,16 @@ __device__ __forceinline__ uint32_t tile_offset(const Operand &o, int r0, int j,
     }
 }
 
+template <class T> using lds_ptr = __attribute__((address_space(3))) T *;
+
+// Orders a wave's own accesses to shared memory.
+__device__ __forceinline__ void wave_lds()
+{
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront", "local");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront", "local");
+}
+
 // Loads 16 bytes a lane straight into shared memory at lds + 16 lane. The
 // caller waits for it (s_waitcnt vmcnt) before the barrier that hands the tile
 // over; the compiler does not see it.
@@ -576,8 +586,11 @@ template <bool PLANES> struct FinishGrad {
     __device__ __forceinline__ void operator()(const Product &a, const Place &at, const Rows<S> &r,
                                                f32x4 (&acc)[S::SP][S::SQ]) const
     {
-        const int w0 = at.p0 + at.wp * (S::SP * 16), v0 = w0 + 8 * (at.lane >> 4);
-        const bool edge = w0 + S::SP * 16 > a.p.rows;
+        constexpr int W = S::SP * 16, LD = W + 8; // a row of the wave's results in shared memory
+        static_assert(16 * LD * 2 <= S::lds / S::waves, "a wave's part of the tiles holds 16 rows");
+        wait_lds_and_meet();
+        const int w0 = at.p0 + at.wp * W, v0 = w0 + 8 * (at.lane >> 4);
+        const bool edge = w0 + W > a.p.rows;
 #pragma unroll
         for (int j = 0; j < S::SQ; ++j) {
             const int t = at.q0 + at.wq * (S::SQ * 16) + j * 16 + (at.lane & 15);
@@ -611,29 +624,33 @@ template <bool PLANES> struct FinishGrad {
                     for (int i = 0; i < 4; ++i)
                         acc[k][j][i] = v0 + class_of(k, i) >= a.p.rows ? 0.0f : acc[k][j][i];
             }
-            uint16_t *to = g + ((int64_t)at.sample * rows_pad + t) * ld + v0;
+            const int q0 = at.q0 + at.wq * (S::SQ * 16) + j * 16;
+            uint16_t *to = g + ((int64_t)at.sample * rows_pad + q0) * ld + w0;
+            const auto write = [&](auto value, uint16_t *out) {
 #pragma unroll
-            for (int k = 0; k < S::SP; k += 2) {
-                if (t >= rows_pad || v0 + k * 16 >= ld)
-                    continue;
-                i16x8 p0;
-                if constexpr (PLANES) {
-                    i16x8 p1, p2;
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const Planes x = planes_of(acc[k + (i >> 2)][j][i & 3]);
-                        p0[i] = (short)x.a;
-                        p1[i] = (short)x.b;
-                        p2[i] = (short)x.c;
-                    }
-                    *(i16x8 *)(to + plane + k * 16) = p1;
-                    *(i16x8 *)(to + 2 * plane + k * 16) = p2;
-                } else {
+                for (int k = 0; k < S::SP; k += 2) {
+                    i16x8 v;
 #pragma unroll
                     for (int i = 0; i < 8; ++i)
-                        p0[i] = (short)ELEM::from(acc[k + (i >> 2)][j][i & 3]);
+                        v[i] = (short)value(acc[k + (i >> 2)][j][i & 3]);
+                    *(lds_ptr<i16x8>)(at.lds + ((at.lane & 15) * LD + k * 16 + 8 * (at.lane >> 4)) * 2) = v;
                 }
-                *(i16x8 *)(to + k * 16) = p0;
+                wave_lds();
+                const int n = min(16, rows_pad - q0) * (W / 8);
+#pragma unroll
+                for (int u = 0; u < W / 32; ++u) {
+                    const int i = at.lane + u * 64, r = i / (W / 8), c = i % (W / 8) * 8;
+                    if (i < n && w0 + c < ld)
+                        *(i16x8 *)(out + (int64_t)r * ld + c) = *(lds_ptr<i16x8>)(at.lds + (r * LD + c) * 2);
+                }
+                wave_lds();
+            };
+            if constexpr (PLANES) {
+                write([](float v) { return planes_of(v).a; }, to);
+                write([](float v) { return planes_of(v).b; }, to + plane);
+                write([](float v) { return planes_of(v).c; }, to + 2 * plane);
+            } else {
+                write([](float v) { return ELEM::from(v); }, to);
             }
             __builtin_amdgcn_sched_barrier(0); // rows side by side would not fit the registers
         }
@@ -650,6 +667,16 @@ template <> __device__ __forceinline__ void put<float>(void *out, int64_t at, fl
 template <class OUT> __device__ __forceinline__ void put4(void *out, int64_t at, f32x4 v)
 {
     *(ushort4 *)((uint16_t *)out + at) = make_ushort4(OUT::from(v[0]), OUT::from(v[1]), OUT::from(v[2]), OUT::from(v[3]));
+}
+template <class OUT> __device__ __forceinline__ void put4(void *out, int64_t at, f32x4 v, f32x4 w)
+{
+    i16x8 x;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        x[i] = (short)OUT::from(v[i]);
+        x[i + 4] = (short)OUT::from(w[i]);
+    }
+    *(i16x8 *)((uint16_t *)out + at) = x;
 }
 template <> __device__ __forceinline__ void put4<float>(void *out, int64_t at, f32x4 v) { *(f32x4 *)((float *)out + at) = v; }
 
@@ -673,63 +700,48 @@ template <class OUT> struct FinishStore {
             const int q = min(at.q0 + at.wq * (S::SQ * 16) + j * 16 + (at.lane & 15), a.q.rows - 1);
             unit[j] = (coef ? coef[(int64_t)at.sample * a.q.rows + q].unit : top->top) * inv_unit;
         }
-        if (a.p.rows % 4 == 0)
-            direct<S>(a, at, unit, acc);
+        constexpr int wide = std::is_same_v<OUT, float> ? 4 : 8; // 16 bytes
+        if (a.p.rows % wide == 0)
+            staged<S, wide>(a, at, unit, acc);
+        else if (a.p.rows % 4 == 0)
+            staged<S, 4>(a, at, unit, acc);
         else
-            staged<S>(a, at, unit, acc);
+            staged<S, 1>(a, at, unit, acc);
     }
-    // Four neighbours at a time.
-    template <class S>
-    __device__ __forceinline__ void direct(const Product &a, const Place &at, const float (&unit)[S::SQ],
-                                           f32x4 (&acc)[S::SP][S::SQ]) const
-    {
-        const int p0 = at.p0 + at.wp * (S::SP * 16) + 4 * (at.lane >> 4);
-#pragma unroll
-        for (int j = 0; j < S::SQ; ++j) {
-            const int q = at.q0 + at.wq * (S::SQ * 16) + j * 16 + (at.lane & 15);
-            if (q >= a.q.rows)
-                continue;
-            const float f = unit[j];
-            const int64_t to = at.sample * sample + (int64_t)q * a.p.rows;
-#pragma unroll
-            for (int k = 0; k < S::SP; ++k) {
-                const int p = p0 + k * 16;
-                if (p < a.p.rows)
-                    put4<OUT>(out, to + p, acc[k][j] * f);
-            }
-        }
-    }
-    // Rows that start at any element: 16 of them pass through shared memory, from
-    // where a wave writes each row's neighbours together (1003 columns of half
-    // precision, 2-byte stores of lanes 8 bytes apart: 163 us for 25000 rows).
-    template <class S>
+    // 16 rows at a time pass through shared memory, from where a wave writes whole
+    // pieces of each row: VEC neighbours a lane.
+    template <class S, int VEC>
     __device__ __forceinline__ void staged(const Product &a, const Place &at, const float (&unit)[S::SQ],
                                            f32x4 (&acc)[S::SP][S::SQ]) const
     {
         constexpr int W = S::SP * 16, LD = W + 4; // a row of the wave's results, in float32
         static_assert(16 * LD * 4 <= S::lds / S::waves, "a wave's part of the tiles holds 16 rows");
         wait_lds_and_meet();
-        auto *row = (__attribute__((address_space(3))) float *)at.lds;
+        const auto row = (lds_ptr<float>)at.lds;
         const int p0 = at.p0 + at.wp * W, q0 = at.q0 + at.wq * (S::SQ * 16);
 #pragma unroll
         for (int j = 0; j < S::SQ; ++j) {
-            const float f = unit[j];
 #pragma unroll
             for (int k = 0; k < S::SP; ++k)
-                *(__attribute__((address_space(3))) f32x4 *)(row + (at.lane & 15) * LD + k * 16 + 4 * (at.lane >> 4)) =
-                    acc[k][j] * f;
-            __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront", "local");
-            __builtin_amdgcn_wave_barrier();
-            __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront", "local");
-            const int n = min(16, a.q.rows - q0 - j * 16);
-            for (int i = at.lane; i < n * W; i += 64) {
-                const int p = p0 + i % W;
-                if (p < a.p.rows)
-                    put<OUT>(out, at.sample * sample + (int64_t)(q0 + j * 16 + i / W) * a.p.rows + p, row[i / W * LD + i % W]);
+                *(lds_ptr<f32x4>)(row + (at.lane & 15) * LD + k * 16 + 4 * (at.lane >> 4)) = acc[k][j] * unit[j];
+            wave_lds();
+            const int n = min(16, a.q.rows - q0 - j * 16) * (W / VEC);
+            const int64_t to = at.sample * sample + (int64_t)(q0 + j * 16) * a.p.rows + p0;
+            for (int i = at.lane; i < n; i += 64) {
+                const int r = i / (W / VEC), c = i % (W / VEC) * VEC;
+                if (p0 + c >= a.p.rows)
+                    continue;
+                const lds_ptr<float> from = row + r * LD + c;
+                const int64_t at_out = to + (int64_t)r * a.p.rows + c;
+                if constexpr (VEC == 8) {
+                    put4<OUT>(out, at_out, *(lds_ptr<f32x4>)from, *(lds_ptr<f32x4>)(from + 4));
+                } else if constexpr (VEC == 4) {
+                    put4<OUT>(out, at_out, *(lds_ptr<f32x4>)from);
+                } else {
+                    put<OUT>(out, at_out, *from);
+                }
             }
-            __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront", "local");
-            __builtin_amdgcn_wave_barrier();
-            __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront", "local");
+            wave_lds();
         }
     }
 };
