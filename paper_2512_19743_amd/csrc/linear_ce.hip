@@ -784,9 +784,120 @@ struct FinishPart {
 // the kernels around the products
 // ---------------------------------------------------------------------------
 
-// Rows copied to dim_pad columns (zeros behind dim) and, where coef is given,
-// rows_out rows a sample with every row times its unit over the largest one (a
-// power of two, so no rounding; zero for ignored rows, whatever they hold).
+// The upstream gradient of row i, times the logits' scale.
+struct Upstream {
+    const float *grad_loss, *total;
+    int reduction;
+    float scale;
+    __device__ __forceinline__ float operator()(int64_t i) const
+    {
+        const float g = grad_loss[reduction == 0 ? i : 0];
+        return (reduction == 2 ? g / total[1] : g) * scale;
+    }
+};
+
+// The largest |b| over the rows that count, of upstream gradients b, and the
+// largest |b| + |c| with the penalty's part c = 2 z_weight lse b.
+__global__ __launch_bounds__(kBlock) void k_ce_size(const CeRow *rows, Targets target, Upstream up, float z_weight,
+                                                    int64_t n, float2 *block_top)
+{
+    __shared__ float2 sm[kBlock / 64];
+    float mb = 0.0f, ms = 0.0f;
+    for (int64_t i = (int64_t)blockIdx.x * kBlock + threadIdx.x; i < n; i += (int64_t)gridDim.x * kBlock) {
+        const float b = up(i), size = fabsf(b) + (z_weight != 0.0f ? fabsf(2.0f * z_weight * rows[i].lse * b) : 0.0f);
+        if (target[i] != kIgnored && size < kInf) {
+            mb = fmaxf(mb, fabsf(b));
+            ms = fmaxf(ms, size);
+        }
+    }
+    for (int o = 32; o > 0; o >>= 1) {
+        mb = fmaxf(mb, __shfl_xor(mb, o));
+        ms = fmaxf(ms, __shfl_xor(ms, o));
+    }
+    if (lane_id() == 0)
+        sm[threadIdx.x >> 6] = make_float2(mb, ms);
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        for (int w = 1; w < kBlock / 64; ++w) {
+            mb = fmaxf(mb, sm[w].x);
+            ms = fmaxf(ms, sm[w].y);
+        }
+        block_top[blockIdx.x] = make_float2(mb, ms);
+    }
+}
+
+// The smallest e with size <= unit 2^e, within [-60, 20].
+__device__ __forceinline__ int exponent_over(float size, float unit)
+{
+    int e = 0;
+    const float f = frexpf(size / unit, &e); // in [1/2, 1)
+    if (f == 0.5f)
+        --e;
+    return size > 0.0f ? min(max(e, -60), 20) : -60;
+}
+
+// The backward pass's coefficients of a row. Its gradient is stored in units of
+// the largest upstream gradient times a power of two, so that it lies in
+// [-1, 1] and equal upstream gradients (a mean) cost the target's value -miss no
+// rounding of their own. tops: k_ce_size's, or 0 of them where all rows have the
+// same upstream gradient and no penalty.
+struct Coefs {
+    const CeRow *rows;
+    Targets target;
+    Upstream up;
+    float z_weight, stored_unit;
+    const float2 *block_top;
+    int tops;
+    // by the whole workgroup
+    __device__ __forceinline__ CeTop top() const
+    {
+        float mb, ms;
+        if (tops == 0) {
+            mb = ms = fabsf(up(0));
+        } else {
+            __shared__ float2 sm[kBlock / 64];
+            mb = ms = 0.0f;
+            for (int i = threadIdx.x; i < tops; i += kBlock) {
+                mb = fmaxf(mb, block_top[i].x);
+                ms = fmaxf(ms, block_top[i].y);
+            }
+            for (int o = 32; o > 0; o >>= 1) {
+                mb = fmaxf(mb, __shfl_xor(mb, o));
+                ms = fmaxf(ms, __shfl_xor(ms, o));
+            }
+            if (lane_id() == 0)
+                sm[threadIdx.x >> 6] = make_float2(mb, ms);
+            __syncthreads();
+            for (int w = 0; w < kBlock / 64; ++w) {
+                mb = fmaxf(mb, sm[w].x);
+                ms = fmaxf(ms, sm[w].y);
+            }
+        }
+        // within 2^+-60: its smallest and largest multiples stay normal
+        const float unit = mb >= 0x1p-60f && mb <= 0x1p60f ? mb : 1.0f;
+        return CeTop{unit, ldexpf(unit, max(exponent_over(ms, unit), 0))};
+    }
+    __device__ __forceinline__ CeCoef operator()(int64_t i, const CeTop &t) const
+    {
+        const int at = target[i];
+        if (at == kIgnored)
+            return CeCoef{0.0f, 0.0f, 0.0f, t.unit};
+        const CeRow r = rows[i];
+        const float b = up(i), c = z_weight != 0.0f ? 2.0f * z_weight * r.lse * b : 0.0f;
+        const float size = fabsf(b) + fabsf(c);
+        const float mine = ldexpf(t.unit, size < kInf ? exponent_over(size, t.unit) : 0);
+        const float bn = b / mine * stored_unit, cn = c / mine * stored_unit;
+        CeCoef k{r.top, (bn + cn) * r.inv_total, cn * (1.0f - r.miss) - bn * r.miss, mine};
+        if (at == kOutside)
+            k.fac = __builtin_nanf("");
+        return k;
+    }
+};
+
+// Rows copied to dim_pad columns (zeros behind dim) and, where scaled, rows_out
+// rows a sample with every row times its unit over the largest one (a power of
+// two, so no rounding; zero for ignored rows, whatever they hold). In the backward
+// pass the first coef_blocks workgroups write the rows' coefficients.
 template <class IN> __device__ __forceinline__ float get(const void *in, int64_t at) { return IN::to(((const uint16_t *)in)[at]); }
 template <> __device__ __forceinline__ float get<float>(const void *in, int64_t at) { return ((const float *)in)[at]; }
 
@@ -800,23 +911,40 @@ struct PackJob {
     uint16_t *out;
     int64_t n;           // elements of one plane of out
     int rows, rows_out;  // per sample
-    const CeCoef *coef;
+    bool scaled;
     unsigned blocks;
 };
 constexpr int kPackJobs = 3;
 struct PackJobs {
     PackJob job[kPackJobs];
     int dim, dim_pad;
-    const CeTop *top;
+    unsigned coef_blocks;
+    int64_t coef_rows;
+    Coefs coefs;
+    CeCoef *coef;
+    CeTop *top;
 };
 
 template <class IN> __global__ __launch_bounds__(kBlock) void k_ce_pack(PackJobs jobs)
 {
     unsigned block = blockIdx.x;
+    if (block < jobs.coef_blocks) {
+        const CeTop top = jobs.coefs.top();
+        if (block == 0 && threadIdx.x == 0)
+            *jobs.top = top;
+        const int64_t i = (int64_t)block * kBlock + threadIdx.x;
+        if (i < jobs.coef_rows)
+            jobs.coef[i] = jobs.coefs(i, top);
+        return;
+    }
+    block -= jobs.coef_blocks;
     int which = 0;
     while (block >= jobs.job[which].blocks)
         block -= jobs.job[which++].blocks;
     const PackJob &p = jobs.job[which];
+    CeTop top{1.0f, 1.0f};
+    if (p.scaled)
+        top = jobs.coefs.top();
     const int64_t i = ((int64_t)block * kBlock + threadIdx.x) * 8;
     if (i >= p.n)
         return;
@@ -827,10 +955,9 @@ template <class IN> __global__ __launch_bounds__(kBlock) void k_ce_pack(PackJobs
     float f = 1.0f;
     bool keep = t < p.rows;
     const int64_t row = sample * p.rows + t;
-    if (p.coef && keep) {
-        const CeCoef c = p.coef[row];
-        keep = c.fac != 0.0f;
-        f = c.unit / jobs.top->top;
+    if (p.scaled && keep) {
+        keep = jobs.coefs.target[row] != kIgnored;
+        f = keep ? jobs.coefs(row, top).unit / top.top : 0.0f;
     }
     float v[8];
     const int64_t at = row * jobs.dim + d;
@@ -1015,127 +1142,38 @@ __global__ __launch_bounds__(kBlock) void k_ce_rows(const float2 *part, int part
     }
 }
 
-// The upstream gradient of row i, times the logits' scale.
-struct Upstream {
-    const float *grad_loss, *total;
-    int reduction;
-    float scale;
-    __device__ __forceinline__ float operator()(int64_t i) const
-    {
-        const float g = grad_loss[reduction == 0 ? i : 0];
-        return (reduction == 2 ? g / total[1] : g) * scale;
-    }
+// Adds up the parts of a gradient and rounds it; one gradient or both.
+struct JoinJob {
+    const float *part;
+    void *out;
+    int64_t rows, split; // elements from one part to the next
+    int splits;
+    const CeCoef *coef;  // grad_x: the rows' units, else NULL
+    unsigned blocks;
 };
-
-// The largest |b| over the rows that count, of upstream gradients b, and the
-// largest |b| + |c| with the penalty's part c = 2 z_weight lse b.
-__global__ __launch_bounds__(kBlock) void k_ce_size(const CeRow *rows, Targets target, Upstream up, float z_weight,
-                                                    int64_t n, float2 *block_top)
+struct JoinJobs {
+    JoinJob job[2];
+    int cols, ld;
+    const CeTop *top;
+    float inv_unit;
+};
+template <class OUT> __global__ __launch_bounds__(kBlock) void k_ce_join(JoinJobs jobs)
 {
-    __shared__ float2 sm[kBlock / 64];
-    float mb = 0.0f, ms = 0.0f;
-    for (int64_t i = (int64_t)blockIdx.x * kBlock + threadIdx.x; i < n; i += (int64_t)gridDim.x * kBlock) {
-        const float b = up(i), size = fabsf(b) + (z_weight != 0.0f ? fabsf(2.0f * z_weight * rows[i].lse * b) : 0.0f);
-        if (target[i] != kIgnored && size < kInf) {
-            mb = fmaxf(mb, fabsf(b));
-            ms = fmaxf(ms, size);
-        }
-    }
-    for (int o = 32; o > 0; o >>= 1) {
-        mb = fmaxf(mb, __shfl_xor(mb, o));
-        ms = fmaxf(ms, __shfl_xor(ms, o));
-    }
-    if (lane_id() == 0)
-        sm[threadIdx.x >> 6] = make_float2(mb, ms);
-    __syncthreads();
-    if (threadIdx.x == 0) {
-        for (int w = 1; w < kBlock / 64; ++w) {
-            mb = fmaxf(mb, sm[w].x);
-            ms = fmaxf(ms, sm[w].y);
-        }
-        block_top[blockIdx.x] = make_float2(mb, ms);
-    }
-}
-
-// The smallest e with size <= unit 2^e, within [-60, 20].
-__device__ __forceinline__ int exponent_over(float size, float unit)
-{
-    int e = 0;
-    const float f = frexpf(size / unit, &e); // in [1/2, 1)
-    if (f == 0.5f)
-        --e;
-    return size > 0.0f ? min(max(e, -60), 20) : -60;
-}
-
-// The backward pass's coefficients of a row. Its gradient is stored in units of
-// the largest upstream gradient times a power of two, so that it lies in
-// [-1, 1] and equal upstream gradients (a mean) cost the target's value -miss no
-// rounding of their own. tops: k_ce_size's, or 0 of them where all rows have the
-// same upstream gradient and no penalty.
-__global__ __launch_bounds__(kBlock) void k_ce_coef(const CeRow *rows, Targets target, Upstream up, float z_weight,
-                                                    float stored_unit, int64_t n, const float2 *block_top, int tops,
-                                                    CeCoef *coef, CeTop *top)
-{
-    __shared__ float2 sm[kBlock / 64];
-    float mb = 0.0f, ms = 0.0f;
-    for (int i = threadIdx.x; i < tops; i += kBlock) {
-        mb = fmaxf(mb, block_top[i].x);
-        ms = fmaxf(ms, block_top[i].y);
-    }
-    for (int o = 32; o > 0; o >>= 1) {
-        mb = fmaxf(mb, __shfl_xor(mb, o));
-        ms = fmaxf(ms, __shfl_xor(ms, o));
-    }
-    if (lane_id() == 0)
-        sm[threadIdx.x >> 6] = make_float2(mb, ms);
-    __syncthreads();
-    for (int w = 0; w < kBlock / 64; ++w) {
-        mb = fmaxf(mb, sm[w].x);
-        ms = fmaxf(ms, sm[w].y);
-    }
-    if (tops == 0)
-        mb = ms = fabsf(up(0));
-    // within 2^+-60: its smallest and largest multiples stay normal
-    const float unit = mb >= 0x1p-60f && mb <= 0x1p60f ? mb : 1.0f;
-    const float largest = ldexpf(unit, max(exponent_over(ms, unit), 0));
-    if (blockIdx.x == 0 && threadIdx.x == 0)
-        *top = CeTop{unit, largest};
-    const int64_t i = (int64_t)blockIdx.x * kBlock + threadIdx.x;
-    if (i >= n)
+    const bool second = blockIdx.x >= jobs.job[0].blocks;
+    const JoinJob &p = jobs.job[second];
+    const int64_t i = ((int64_t)(blockIdx.x - (second ? jobs.job[0].blocks : 0)) * kBlock + threadIdx.x) * 4;
+    const int64_t r = i / jobs.ld;
+    const int c = (int)(i - r * jobs.ld);
+    if (r >= p.rows)
         return;
-    const CeRow r = rows[i];
-    const int t = target[i];
-    const float b = up(i), c = z_weight != 0.0f ? 2.0f * z_weight * r.lse * b : 0.0f;
-    const float size = fabsf(b) + fabsf(c);
-    const float mine = ldexpf(unit, size < kInf ? exponent_over(size, unit) : 0);
-    const float bn = b / mine * stored_unit, cn = c / mine * stored_unit;
-    CeCoef k{r.top, (bn + cn) * r.inv_total, cn * (1.0f - r.miss) - bn * r.miss, mine};
-    if (t == kIgnored)
-        k = CeCoef{0.0f, 0.0f, 0.0f, unit};
-    if (t == kOutside)
-        k.fac = __builtin_nanf("");
-    coef[i] = k;
-}
-
-// Adds up the parts of a gradient and rounds it.
-template <class OUT>
-__global__ __launch_bounds__(kBlock) void k_ce_join(const float *part, int splits, int64_t split, int cols, int ld,
-                                                    int64_t rows, const CeCoef *coef, const CeTop *top, float inv_unit,
-                                                    void *out)
-{
-    const int64_t i = ((int64_t)blockIdx.x * kBlock + threadIdx.x) * 4;
-    const int64_t r = i / ld;
-    const int c = (int)(i - r * ld);
-    if (r >= rows)
-        return;
-    f32x4 v = *(const f32x4 *)(part + i);
-    for (int s = 1; s < splits; ++s)
-        v += *(const f32x4 *)(part + s * split + i);
-    v *= (coef ? coef[r].unit : top->top) * inv_unit;
+    f32x4 v = *(const f32x4 *)(p.part + i);
+    for (int s = 1; s < p.splits; ++s)
+        v += *(const f32x4 *)(p.part + s * p.split + i);
+    v *= (p.coef ? p.coef[r].unit : jobs.top->top) * jobs.inv_unit;
 #pragma unroll
     for (int u = 0; u < 4; ++u)
-        if (c + u < cols)
-            put<OUT>(out, r * cols + c + u, v[u]);
+        if (c + u < jobs.cols)
+            put<OUT>(p.out, r * jobs.cols + c + u, v[u]);
 }
 
 // ---------------------------------------------------------------------------
@@ -1266,7 +1304,7 @@ struct Packs {
     PackJobs jobs{};
     int n = 0;
     unsigned blocks = 0;
-    void add(const void *in, uint16_t *out, int64_t samples, int rows, int rows_out, const CeCoef *coef)
+    void add(const void *in, uint16_t *out, int64_t samples, int rows, int rows_out, bool scaled)
     {
         PackJob &j = jobs.job[n++];
         j.in = in;
@@ -1274,13 +1312,13 @@ struct Packs {
         j.n = samples * rows_out * jobs.dim_pad;
         j.rows = rows;
         j.rows_out = rows_out;
-        j.coef = coef;
+        j.scaled = scaled;
         j.blocks = blocks_for(j.n / 8, kBlock);
         blocks += j.blocks;
     }
     template <class IN> void launch(hipStream_t s) const
     {
-        if (n)
+        if (blocks)
             k_ce_pack<IN><<<dim3(blocks), dim3(kBlock), 0, s>>>(jobs);
     }
 };
@@ -1292,6 +1330,22 @@ float scale2_of(const CeProblem &p)
     const float s = p.scale * kLog2E;
     return std::abs(s) < FLT_MIN ? std::copysign(FLT_MIN, s) : s;
 }
+
+// Gradients whose parts wait to be added up.
+struct Joins {
+    JoinJobs jobs{};
+    int n = 0;
+    void add(const float *part, void *out, int64_t rows, int64_t split, int splits, const CeCoef *coef)
+    {
+        jobs.job[n++] = JoinJob{part, out, rows, split, splits, coef, blocks_for(rows * jobs.ld / 4, kBlock)};
+    }
+    template <class OUT> void launch(hipStream_t s)
+    {
+        if (n)
+            k_ce_join<OUT><<<dim3(jobs.job[0].blocks + (n > 1 ? jobs.job[1].blocks : 0)), dim3(kBlock), 0, s>>>(jobs);
+        n = 0;
+    }
+};
 
 Targets targets_of(const CeProblem &p) { return {p.target, p.target32, p.classes, p.ignore_index}; }
 
@@ -1362,9 +1416,9 @@ void ce_forward(const CeProblem &p, const CeForwardPlan &plan, uint8_t *ws, floa
         packs.jobs.dim = p.dim;
         packs.jobs.dim_pad = plan.dim_pad;
         if (plan.pack_x)
-            packs.add(p.x, x, p.samples, p.rows, p.rows, nullptr);
+            packs.add(p.x, x, p.samples, p.rows, p.rows, false);
         if (plan.pack_w)
-            packs.add(p.w, w, p.samples, p.classes, p.classes, nullptr);
+            packs.add(p.w, w, p.samples, p.classes, p.classes, false);
         packs.launch<IO>(s);
         Product a{};
         a.p = features(p, plan.pack_w, p.w, w, p.classes, plan.dim_pad);
@@ -1467,21 +1521,28 @@ void ce_backward(const CeProblem &p, const CeBackwardPlan &plan, uint8_t *ws, co
         const float inv_unit = 1.0f / ELEM::kUnit;
         if (plan.tops)
             k_ce_size<<<dim3(plan.tops), dim3(kBlock), 0, s>>>(rows, target, up, p.z_weight, n, block_top);
-        k_ce_coef<<<dim3(blocks_for(n, kBlock)), dim3(kBlock), 0, s>>>(rows, target, up, p.z_weight, ELEM::kUnit, n,
-                                                                      block_top, plan.tops, coef, top);
         Packs packs;
         packs.jobs.dim = p.dim;
         packs.jobs.dim_pad = plan.dim_pad;
+        packs.jobs.coefs = Coefs{rows, target, up, p.z_weight, ELEM::kUnit, block_top, plan.tops};
+        packs.jobs.coef_rows = n;
+        packs.jobs.coef = coef;
         packs.jobs.top = top;
+        packs.blocks = packs.jobs.coef_blocks = blocks_for(n, kBlock);
         if (plan.pack_x)
-            packs.add(p.x, x, p.samples, p.rows, p.rows, nullptr);
+            packs.add(p.x, x, p.samples, p.rows, p.rows, false);
         if (plan.pack_w)
-            packs.add(p.w, w, p.samples, p.classes, p.classes, nullptr);
+            packs.add(p.w, w, p.samples, p.classes, p.classes, false);
         if (grad_w)
-            packs.add(p.x, xs, p.samples, p.rows, plan.rows_pad, coef);
+            packs.add(p.x, xs, p.samples, p.rows, plan.rows_pad, true);
         packs.launch<IO>(s);
         const Operand W = features(p, plan.pack_w, p.w, w, p.classes, plan.dim_pad);
         const Operand X = features(p, plan.pack_x, p.x, x, p.rows, plan.dim_pad);
+        Joins joins;
+        joins.jobs.cols = p.dim;
+        joins.jobs.ld = (int)ld;
+        joins.jobs.top = top;
+        joins.jobs.inv_unit = inv_unit;
         for (int s0 = 0; s0 < p.samples; s0 += plan.piece_samples) {
             const int ns = std::min(plan.piece_samples, p.samples - s0);
             for (int c0 = 0; c0 < p.classes; c0 += plan.piece_classes) {
@@ -1503,6 +1564,7 @@ void ce_backward(const CeProblem &p, const CeBackwardPlan &plan, uint8_t *ws, co
                         choose(nc, p.rows, ns, false), a, nc_pad, plan.rows_pad,
                         FinishGrad<PLANES>{target, coef, r0, g, plane_g, scale2_of(p), plan.rows_pad, plan.ld_g, c0}, s);
                 }
+                joins.launch<IO>(s); // the last piece's, before its parts are written over
                 Operand G;
                 G.base = g;
                 G.sample = (int64_t)plan.rows_pad * plan.ld_g;
@@ -1557,8 +1619,7 @@ void ce_backward(const CeProblem &p, const CeBackwardPlan &plan, uint8_t *ws, co
                         launch_product<ELEM, PLANES, true, true>(kind, a, p.dim, nc,
                                                                  FinishPart{part_w, split, per, (int)ld, false}, s);
                         // several samples only where a piece holds all their classes
-                        k_ce_join<IO><<<dim3(blocks_for(split / 4, kBlock)), dim3(kBlock), 0, s>>>(
-                            part_w, plan.split_w, split, p.dim, (int)ld, (int64_t)ns * nc, nullptr, top, inv_unit, to);
+                        joins.add(part_w, to, (int64_t)ns * nc, split, plan.split_w, nullptr);
                     } else {
                         launch_product<ELEM, PLANES, true, true>(kind, a, p.dim, nc,
                                                                  FinishStore<IO>{to, nullptr, top, inv_unit, sample}, s);
@@ -1567,11 +1628,11 @@ void ce_backward(const CeProblem &p, const CeBackwardPlan &plan, uint8_t *ws, co
             }
             if (grad_x && plan.sum_x) {
                 const int64_t sample = (int64_t)p.rows * ld, split = plan.piece_samples * sample;
-                k_ce_join<IO><<<dim3(blocks_for(ns * sample / 4, kBlock)), dim3(kBlock), 0, s>>>(
-                    part_x, plan.split_x, split, p.dim, (int)ld, (int64_t)ns * p.rows, coef + (int64_t)s0 * p.rows, top,
-                    inv_unit, (uint8_t *)grad_x + (int64_t)s0 * p.rows * p.dim * elem_size(p.type));
+                joins.add(part_x, (uint8_t *)grad_x + (int64_t)s0 * p.rows * p.dim * elem_size(p.type),
+                          (int64_t)ns * p.rows, split, plan.split_x, coef + (int64_t)s0 * p.rows);
             }
         }
+        joins.launch<IO>(s);
     });
 }
 
