@@ -80,6 +80,8 @@ _lock = threading.Lock()
 def load() -> ctypes.CDLL:
     """Loads libapml.so from the package directory (built by build_lib.build())."""
     global _lib
+    if _lib is not None:
+        return _lib
     with _lock:
         if _lib is not None:
             return _lib
@@ -394,16 +396,18 @@ _INDEX_TYPES = {torch.int64: 0, torch.int32: 1}
 _REDUCTIONS = {"none": 0, "sum": 1, "mean": 2}
 
 
-def _on_gpu(name: str, t: torch.Tensor, types, like: Optional[torch.Tensor] = None) -> torch.Tensor:
+def _on_gpu(name: str, t: torch.Tensor, types, device: Optional[int] = None) -> int:
+    """Checks a tensor of a call; returns its device's index."""
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise ValueError(f"{name} must be a tensor on a GPU (libapml has no CPU path)")
     if t.dtype not in types:
         raise ValueError(f"{name} must be {' or '.join(str(d).replace('torch.', '') for d in types)}, got {t.dtype}")
     if not t.is_contiguous():
         raise ValueError(f"{name} must be contiguous")
-    if like is not None and t.device != like.device:
-        raise ValueError(f"{name} must be on {like.device}, got {t.device}")
-    return t
+    at = t.get_device()
+    if device is not None and at != device:
+        raise ValueError(f"{name} must be on cuda:{device}, got {t.device}")
+    return at
 
 
 def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
@@ -415,20 +419,19 @@ class _Queued:
 
     __slots__ = ("guard", "device", "stream")
 
-    def __init__(self, device: torch.device, stream: Optional[torch.cuda.Stream]):
-        self.guard = None
+    def __init__(self, like: torch.Tensor, stream: Optional[torch.cuda.Stream]):
+        self.guard, self.device, self.stream = None, like.get_device(), stream
         if stream is not None:
-            if stream.device != device:
-                raise ValueError(f"stream must be on {device}, got {stream.device}")
+            if stream.device != like.device:
+                raise ValueError(f"stream must be on {like.device}, got {stream.device}")
             self.guard = torch.cuda.stream(stream)
-        elif torch.cuda.current_device() != device.index:
-            self.guard = torch.cuda.device(device)
-        self.device, self.stream = device, stream
+        elif torch.cuda.current_device() != self.device:
+            self.guard = torch.cuda.device(self.device)
 
     def __enter__(self):
         if self.guard is not None:
             self.guard.__enter__()
-        return _stream_handle(self.stream, self.device)
+        return self.stream.cuda_stream if self.stream is not None else torch.cuda.current_stream(self.device).cuda_stream
 
     def __exit__(self, *exc):
         if self.guard is not None:
@@ -463,26 +466,58 @@ def _ce_workspace(d, x, w, backward: bool) -> torch.Tensor:
 
 
 def _linear_ce_desc(x, w, target, scale, z_weight, ignore_index, reduction) -> apml_linear_ce_desc:
-    _on_gpu("x", x, _DTYPES)
-    _on_gpu("w", w, (x.dtype,), x)
-    _on_gpu("target", target, _INDEX_TYPES, x)
+    device = _on_gpu("x", x, _DTYPES)
+    _on_gpu("w", w, (x.dtype,), device)
+    _on_gpu("target", target, _INDEX_TYPES, device)
     if reduction not in _REDUCTIONS:
         raise ValueError(f"unknown reduction {reduction!r}")
-    if w.dim() not in (2, 3) or x.dim() < 2 or (w.dim() == 3 and (x.dim() != 3 or x.shape[0] != w.shape[0])):
+    xs, ws = x.shape, w.shape
+    if len(ws) not in (2, 3) or len(xs) < 2 or (len(ws) == 3 and (len(xs) != 3 or xs[0] != ws[0])):
         raise ValueError("need x (..., dim) with w (classes, dim), or x (B, rows, dim) with w (B, classes, dim)")
-    if x.shape[-1] != w.shape[-1]:
+    if xs[-1] != ws[-1]:
         raise ValueError("x and w must have the same dim")
-    if target.shape != x.shape[:-1]:
+    if target.shape != xs[:-1]:
         raise ValueError("target must have x's shape without its last dimension")
-    if w.shape[-2] < 1 or x.shape[-1] < 1:
+    if ws[-2] < 1 or xs[-1] < 1:
         raise ValueError("need at least one class and dim >= 1")
-    samples = w.shape[0] if w.dim() == 3 else 1
+    samples = ws[0] if len(ws) == 3 else 1
     # no row: the caller launches nothing
     rows = target.numel() // samples if samples else 0
-    if max(samples, rows, w.shape[-2], x.shape[-1]) >= 1 << 31:
+    if max(samples, rows, ws[-2], xs[-1]) >= 1 << 31:
         raise ValueError("a size is beyond the library's 32-bit range")
     return apml_linear_ce_desc(ctypes.sizeof(apml_linear_ce_desc), _DTYPES[x.dtype], _INDEX_TYPES[target.dtype], samples,
-                               rows, w.shape[-2], x.shape[-1], _REDUCTIONS[reduction], scale, z_weight, ignore_index)
+                               rows, ws[-2], xs[-1], _REDUCTIONS[reduction], scale, z_weight, ignore_index)
+
+
+def _linear_ce_forward(d, x, w, target, keep_state, stream=None):
+    shape = target.shape if d.reduction == 0 else ()
+    with _Queued(x, stream) as queue:
+        if d.rows == 0:
+            return x.new_zeros(shape, dtype=torch.float32), x.new_empty((0, 4), dtype=torch.float32)
+        loss = torch.empty(shape, dtype=torch.float32, device=x.device)
+        state = None
+        if keep_state:
+            state = torch.empty(d.samples * d.rows + 1, 4, dtype=torch.float32, device=x.device)
+        ws = _ce_workspace(d, x, w, False)
+        st = load().apml_linear_ce_forward(ctypes.byref(d), x.data_ptr(), w.data_ptr(), target.data_ptr(),
+                                           loss.data_ptr(), _ptr(state), ws.data_ptr(), ws.numel(), queue)
+    _check("apml_linear_ce_forward", st)
+    return loss, state
+
+
+def _linear_ce_backward(d, state, x, w, target, grad_loss, want_x, want_w, stream=None):
+    with _Queued(x, stream) as queue:
+        make = torch.empty_like if d.rows else torch.zeros_like
+        gx = make(x) if want_x else None
+        gw = make(w) if want_w else None
+        if d.rows == 0:
+            return gx, gw
+        ws = _ce_workspace(d, x, w, True)
+        st = load().apml_linear_ce_backward(ctypes.byref(d), x.data_ptr(), w.data_ptr(), target.data_ptr(),
+                                            state.data_ptr(), grad_loss.data_ptr(), _ptr(gx), _ptr(gw), ws.data_ptr(),
+                                            ws.numel(), queue)
+    _check("apml_linear_ce_backward", st)
+    return gx, gw
 
 
 def apml_linear_ce_forward(x: torch.Tensor, w: torch.Tensor, target: torch.Tensor, *, scale: float = 1.0,
@@ -496,19 +531,8 @@ def apml_linear_ce_forward(x: torch.Tensor, w: torch.Tensor, target: torch.Tenso
     classes of its own. float32, bfloat16 or float16; target int64 or int32, of x's leading shape.
     """
     d = _linear_ce_desc(x, w, target, scale, z_weight, ignore_index, reduction)
-    with _Queued(x.device, stream) as queue:
-        state = None
-        if d.rows == 0:
-            loss = torch.zeros(target.shape if reduction == "none" else (), dtype=torch.float32, device=x.device)
-            return loss, torch.empty(0, 4, dtype=torch.float32, device=x.device) if keep_state else None
-        loss = torch.empty(target.shape if reduction == "none" else (), dtype=torch.float32, device=x.device)
-        if keep_state:
-            state = torch.empty(d.samples * d.rows + 1, 4, dtype=torch.float32, device=x.device)
-        ws = _ce_workspace(d, x, w, False)
-        st = load().apml_linear_ce_forward(ctypes.byref(d), _ptr(x), _ptr(w), _ptr(target), _ptr(loss), _ptr(state),
-                                           _ptr(ws), ws.numel(), queue)
-    _check("apml_linear_ce_forward", st)
-    return loss, state
+    loss, state = _linear_ce_forward(d, x, w, target, keep_state, stream)
+    return loss, state if keep_state else None
 
 
 def apml_linear_ce_backward(state: torch.Tensor, x: torch.Tensor, w: torch.Tensor, target: torch.Tensor,
@@ -518,25 +542,15 @@ def apml_linear_ce_backward(state: torch.Tensor, x: torch.Tensor, w: torch.Tenso
                             ) -> Tuple[Optional[torch.Tensor], Optional[torch.Tensor]]:
     """Gradients of sum(grad_loss * loss) in x's type; the other arguments as in the forward call."""
     d = _linear_ce_desc(x, w, target, scale, z_weight, ignore_index, reduction)
-    _on_gpu("grad_loss", grad_loss, (torch.float32,), x)
-    _on_gpu("state", state, (torch.float32,), x)
+    _on_gpu("grad_loss", grad_loss, (torch.float32,), x.get_device())
+    _on_gpu("state", state, (torch.float32,), x.get_device())
     if grad_loss.numel() != (target.numel() if reduction == "none" else 1):
         raise ValueError("grad_loss must have the loss's shape")
     if not (want_grad_x or want_grad_w):
         return None, None
     if d.rows and state.numel() != 4 * (d.samples * d.rows + 1):
         raise ValueError("state must come from the forward call on the same shapes")
-    with _Queued(x.device, stream) as queue:
-        make = torch.empty_like if d.rows else torch.zeros_like
-        gx = make(x) if want_grad_x else None
-        gw = make(w) if want_grad_w else None
-        if d.rows == 0:
-            return gx, gw
-        ws = _ce_workspace(d, x, w, True)
-        st = load().apml_linear_ce_backward(ctypes.byref(d), _ptr(x), _ptr(w), _ptr(target), _ptr(state),
-                                            _ptr(grad_loss), _ptr(gx), _ptr(gw), _ptr(ws), ws.numel(), queue)
-    _check("apml_linear_ce_backward", st)
-    return gx, gw
+    return _linear_ce_backward(d, state, x, w, target, grad_loss, want_grad_x, want_grad_w, stream)
 
 
 def _routed(shape, what: str, t: torch.Tensor, lead) -> None:
@@ -545,7 +559,7 @@ def _routed(shape, what: str, t: torch.Tensor, lead) -> None:
 
 
 def _balance_desc(logits, index, valid, z_weight, reduction) -> apml_balance_desc:
-    _on_gpu("logits", logits, _DTYPES)
+    device = _on_gpu("logits", logits, _DTYPES)
     if reduction not in _REDUCTIONS:
         raise ValueError(f"unknown reduction {reduction!r}")
     if logits.dim() not in (2, 3):
@@ -554,13 +568,13 @@ def _balance_desc(logits, index, valid, z_weight, reduction) -> apml_balance_des
     samples, tokens, experts = lead[0] if logits.dim() == 3 else 1, lead[-1], logits.shape[-1]
     chosen, index_type = 1, torch.int64
     if index is not None:
-        _on_gpu("experts", index, _INDEX_TYPES, logits)
+        _on_gpu("experts", index, _INDEX_TYPES, device)
         _routed(logits.dim(), "experts", index, lead)
         chosen, index_type = index.shape[-1], index.dtype
         if chosen < 1:
             raise ValueError("experts must name at least one expert a token")
     if valid is not None:
-        _on_gpu("valid", valid, (torch.bool,), logits)
+        _on_gpu("valid", valid, (torch.bool,), device)
         _routed(logits.dim() - 1, "valid", valid, lead)
     if experts < 1 or samples < 1:
         raise ValueError("need at least one sample and one expert")
@@ -568,6 +582,47 @@ def _balance_desc(logits, index, valid, z_weight, reduction) -> apml_balance_des
         raise ValueError("a size is beyond the library's 32-bit range")
     return apml_balance_desc(ctypes.sizeof(apml_balance_desc), _DTYPES[logits.dtype], _INDEX_TYPES[index_type], samples,
                              tokens, experts, chosen, _REDUCTIONS[reduction], z_weight)
+
+
+def _balance_counts(logits, experts, counts) -> None:
+    if (experts is None) == (counts is None):
+        raise ValueError("give either experts or counts")
+    if counts is not None:
+        _on_gpu("counts", counts, (torch.int64,), logits.get_device())
+        shape = logits.shape[:-2] + logits.shape[-1:]
+        if counts.shape != shape:
+            raise ValueError(f"counts must have the shape {tuple(shape)}")
+
+
+def _balance_forward(d, logits, experts, counts, valid, keep_state, stream=None):
+    shape = logits.shape[:-2] if d.reduction == 0 else ()
+    with _Queued(logits, stream) as queue:
+        device = logits.device
+        if counts is None:
+            make = torch.empty if d.tokens else torch.zeros
+            counts = make(logits.shape[:-2] + logits.shape[-1:], dtype=torch.int64, device=device)
+        if d.tokens == 0:
+            return logits.new_zeros(shape, dtype=torch.float32), counts, logits.new_empty(0, dtype=torch.float32)
+        loss = torch.empty(shape, dtype=torch.float32, device=device)
+        state = torch.empty(d.samples, d.experts + 1, dtype=torch.float32, device=device) if keep_state else None
+        ws = _workspace(("balance", d.dtype, d.samples, d.tokens, d.experts), device, lambda n: _check(
+            "apml_balance_workspace", load().apml_balance_workspace(ctypes.byref(d), n)))
+        st = load().apml_balance_forward(ctypes.byref(d), logits.data_ptr(), _ptr(experts), _ptr(valid),
+                                         counts.data_ptr(), loss.data_ptr(), _ptr(state), ws.data_ptr(), ws.numel(),
+                                         queue)
+    _check("apml_balance_forward", st)
+    return loss, counts, state
+
+
+def _balance_backward(d, state, logits, valid, grad_loss, stream=None):
+    with _Queued(logits, stream) as queue:
+        grad = torch.empty_like(logits)
+        if d.tokens == 0:
+            return grad
+        st = load().apml_balance_backward(ctypes.byref(d), logits.data_ptr(), _ptr(valid), state.data_ptr(),
+                                          grad_loss.data_ptr(), grad.data_ptr(), queue)
+    _check("apml_balance_backward", st)
+    return grad
 
 
 def apml_balance_forward(logits: torch.Tensor, experts: Optional[torch.Tensor] = None, *,
@@ -582,31 +637,10 @@ def apml_balance_forward(logits: torch.Tensor, experts: Optional[torch.Tensor] =
     of each token, or counts (B, experts) or (experts,): their tokens, int64; valid: bool, the tokens'
     shape, False for padding.
     """
-    if (experts is None) == (counts is None):
-        raise ValueError("give either experts or counts")
     d = _balance_desc(logits, experts, valid, z_weight, reduction)
-    shape = logits.shape[:-2] + logits.shape[-1:]
-    if counts is not None:
-        _on_gpu("counts", counts, (torch.int64,), logits)
-        if counts.shape != shape:
-            raise ValueError(f"counts must have the shape {tuple(shape)}")
-    with _Queued(logits.device, stream) as queue:
-        lead = logits.shape[:-2] if reduction == "none" else ()
-        if d.tokens == 0:
-            if counts is None:
-                counts = torch.zeros(shape, dtype=torch.int64, device=logits.device)
-            loss = torch.zeros(lead, dtype=torch.float32, device=logits.device)
-            return loss, counts, torch.empty(0, dtype=torch.float32, device=logits.device) if keep_state else None
-        loss = torch.empty(lead, dtype=torch.float32, device=logits.device)
-        if counts is None:
-            counts = torch.empty(shape, dtype=torch.int64, device=logits.device)
-        state = torch.empty(d.samples, d.experts + 1, dtype=torch.float32, device=logits.device) if keep_state else None
-        ws = _workspace(("balance", d.dtype, d.samples, d.tokens, d.experts), logits.device, lambda n: _check(
-            "apml_balance_workspace", load().apml_balance_workspace(ctypes.byref(d), n)))
-        st = load().apml_balance_forward(ctypes.byref(d), _ptr(logits), _ptr(experts), _ptr(valid), _ptr(counts),
-                                         _ptr(loss), _ptr(state), _ptr(ws), ws.numel(), queue)
-    _check("apml_balance_forward", st)
-    return loss, counts, state
+    _balance_counts(logits, experts, counts)
+    loss, counts, state = _balance_forward(d, logits, experts, counts, valid, keep_state, stream)
+    return loss, counts, state if keep_state else None
 
 
 def apml_balance_backward(state: torch.Tensor, logits: torch.Tensor, grad_loss: torch.Tensor, *,
@@ -614,20 +648,13 @@ def apml_balance_backward(state: torch.Tensor, logits: torch.Tensor, grad_loss: 
                           stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
     """Gradient of sum(grad_loss * loss) in logits' type; the other arguments as in the forward call."""
     d = _balance_desc(logits, None, valid, z_weight, reduction)
-    _on_gpu("grad_loss", grad_loss, (torch.float32,), logits)
-    _on_gpu("state", state, (torch.float32,), logits)
+    _on_gpu("grad_loss", grad_loss, (torch.float32,), logits.get_device())
+    _on_gpu("state", state, (torch.float32,), logits.get_device())
     if grad_loss.numel() != (d.samples if reduction == "none" else 1):
         raise ValueError("grad_loss must have the loss's shape")
     if d.tokens and state.numel() != d.samples * (d.experts + 1):
         raise ValueError("state must come from the forward call on the same shapes")
-    with _Queued(logits.device, stream) as queue:
-        grad = torch.empty_like(logits)
-        if d.tokens == 0:
-            return grad
-        st = load().apml_balance_backward(ctypes.byref(d), _ptr(logits), _ptr(valid), _ptr(state), _ptr(grad_loss),
-                                          _ptr(grad), queue)
-    _check("apml_balance_backward", st)
-    return grad
+    return _balance_backward(d, state, logits, valid, grad_loss, stream)
 
 
 def apml_expert_counts(experts: torch.Tensor, num_experts: int, *, valid: Optional[torch.Tensor] = None,
@@ -635,16 +662,16 @@ def apml_expert_counts(experts: torch.Tensor, num_experts: int, *, valid: Option
     """Tokens per expert, int64: (B, num_experts) for experts (B, tokens, chosen), (num_experts,) for
     (tokens, chosen). Entries outside [0, num_experts) are dropped slots; tokens that are not valid are
     padding."""
-    _on_gpu("experts", experts, _INDEX_TYPES)
+    device = _on_gpu("experts", experts, _INDEX_TYPES)
     if experts.dim() not in (2, 3):
         raise ValueError("experts must be (tokens, chosen) or (B, tokens, chosen)")
     if valid is not None:
-        _on_gpu("valid", valid, (torch.bool,), experts)
+        _on_gpu("valid", valid, (torch.bool,), device)
         _routed(experts.dim() - 1, "valid", valid, experts.shape[:-1])
     if max(*experts.shape, num_experts) >= 1 << 31 or num_experts < 1:
         raise ValueError("num_experts must be at least 1, and every size below 2^31")
     samples = experts.shape[0] if experts.dim() == 3 else 1
-    with _Queued(experts.device, stream) as queue:
+    with _Queued(experts, stream) as queue:
         shape = experts.shape[:-2] + (num_experts,)
         if experts.numel() == 0:
             return torch.zeros(shape, dtype=torch.int64, device=experts.device)

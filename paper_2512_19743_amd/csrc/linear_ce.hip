@@ -1564,7 +1564,6 @@ void ce_backward(const CeProblem &p, const CeBackwardPlan &plan, uint8_t *ws, co
                         choose(nc, p.rows, ns, false), a, nc_pad, plan.rows_pad,
                         FinishGrad<PLANES>{target, coef, r0, g, plane_g, scale2_of(p), plan.rows_pad, plan.ld_g, c0}, s);
                 }
-                joins.launch<IO>(s); // the last piece's, before its parts are written over
                 Operand G;
                 G.base = g;
                 G.sample = (int64_t)plan.rows_pad * plan.ld_g;
@@ -1620,6 +1619,8 @@ void ce_backward(const CeProblem &p, const CeBackwardPlan &plan, uint8_t *ws, co
                                                                  FinishPart{part_w, split, per, (int)ld, false}, s);
                         // several samples only where a piece holds all their classes
                         joins.add(part_w, to, (int64_t)ns * nc, split, plan.split_w, nullptr);
+                        if (c0 + plan.piece_classes < p.classes)
+                            joins.launch<IO>(s); // before its parts are written over
                     } else {
                         launch_product<ELEM, PLANES, true, true>(kind, a, p.dim, nc,
                                                                  FinishStore<IO>{to, nullptr, top, inv_unit, sample}, s);
@@ -1631,8 +1632,8 @@ void ce_backward(const CeProblem &p, const CeBackwardPlan &plan, uint8_t *ws, co
                 joins.add(part_x, (uint8_t *)grad_x + (int64_t)s0 * p.rows * p.dim * elem_size(p.type),
                           (int64_t)ns * p.rows, split, plan.split_x, coef + (int64_t)s0 * p.rows);
             }
+            joins.launch<IO>(s); // while its parts are in the cache
         }
-        joins.launch<IO>(s);
     });
 }
 

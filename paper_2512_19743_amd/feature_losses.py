@@ -9,24 +9,34 @@ from torch.autograd.function import once_differentiable
 from . import _lib
 
 
+def _upstream(grad_loss: torch.Tensor) -> torch.Tensor:
+    return grad_loss if grad_loss.dtype == torch.float32 and grad_loss.is_contiguous() else \
+        grad_loss.to(torch.float32).contiguous()
+
+
+def _linear_ce_grads(ctx, grad_loss):
+    x, w, target, state = ctx.saved_tensors
+    want_x, want_w = ctx.needs_input_grad[:2]
+    gx, gw = _lib._linear_ce_backward(ctx.desc, state, x, w, target, _upstream(grad_loss), want_x, want_w)
+    return gx, gw, None, None
+
+
 class LinearCEFunction(torch.autograd.Function):
     """Softmax cross entropy against classes; the logits are computed again in backward, never kept."""
 
     @staticmethod
-    def forward(ctx, x, w, target, keywords):
-        loss, state = _lib.apml_linear_ce_forward(x, w, target, keep_state=any(ctx.needs_input_grad[:2]), **keywords)
-        ctx.keywords = keywords
+    def forward(ctx, x, w, target, desc):
+        need = ctx.needs_input_grad
+        loss, state = _lib._linear_ce_forward(desc, x, w, target, need[0] or need[1])
+        ctx.desc = desc
         ctx.save_for_backward(x, w, target, state)
         return loss
 
     @staticmethod
-    @once_differentiable
     def backward(ctx, grad_loss):
-        x, w, target, state = ctx.saved_tensors
-        gx, gw = _lib.apml_linear_ce_backward(state, x, w, target, grad_loss.contiguous().to(torch.float32),
-                                              want_grad_x=ctx.needs_input_grad[0], want_grad_w=ctx.needs_input_grad[1],
-                                              **ctx.keywords)
-        return gx, gw, None, None
+        if torch.is_grad_enabled():  # create_graph: a second derivative is refused, where one is asked for
+            return once_differentiable(_linear_ce_grads)(ctx, grad_loss)
+        return _linear_ce_grads(ctx, grad_loss)
 
 
 def linear_ce_loss(x: torch.Tensor, w: torch.Tensor, target: torch.Tensor, *, scale: float = 1.0,
@@ -41,31 +51,35 @@ def linear_ce_loss(x: torch.Tensor, w: torch.Tensor, target: torch.Tensor, *, sc
     z_weight: weight of the squared log-sum-exp that is added per row.
     reduction: 'none' (target's shape), 'sum', or 'mean' over the rows that are not ignored.
     """
-    keywords = dict(scale=scale, z_weight=z_weight, ignore_index=ignore_index, reduction=reduction)
-    return LinearCEFunction.apply(x.contiguous(), w.contiguous(), target.contiguous(), keywords)
+    x, w, target = x.contiguous(), w.contiguous(), target.contiguous()
+    desc = _lib._linear_ce_desc(x, w, target, scale, z_weight, ignore_index, reduction)
+    return LinearCEFunction.apply(x, w, target, desc)
+
+
+def _balance_grads(ctx, grad_loss, _):
+    logits, valid, state = ctx.saved_tensors
+    grad = _lib._balance_backward(ctx.desc, state, logits, valid, _upstream(grad_loss))
+    return grad, None, None, None, None
 
 
 class BalanceFunction(torch.autograd.Function):
     """Balance loss of routed experts and the tokens per expert; the softmax is computed again in backward."""
 
     @staticmethod
-    def forward(ctx, logits, experts, counts, valid, z_weight, reduction):
-        loss, got, state = _lib.apml_balance_forward(logits, experts, counts=counts, valid=valid, z_weight=z_weight,
-                                                     reduction=reduction, keep_state=ctx.needs_input_grad[0])
-        ctx.z_weight, ctx.reduction = z_weight, reduction
+    def forward(ctx, logits, experts, counts, valid, desc):
+        loss, got, state = _lib._balance_forward(desc, logits, experts, counts, valid, ctx.needs_input_grad[0])
+        ctx.desc = desc
         ctx.save_for_backward(logits, valid, state)
         if counts is not None:  # an input is no output
-            got = torch.empty(0, dtype=torch.int64, device=logits.device)
+            got = logits.new_empty(0, dtype=torch.int64)
         ctx.mark_non_differentiable(got)
         return loss, got
 
     @staticmethod
-    @once_differentiable
-    def backward(ctx, grad_loss, _):
-        logits, valid, state = ctx.saved_tensors
-        grad = _lib.apml_balance_backward(state, logits, grad_loss.contiguous().to(torch.float32), valid=valid,
-                                          z_weight=ctx.z_weight, reduction=ctx.reduction)
-        return grad, None, None, None, None, None
+    def backward(ctx, grad_loss, grad_counts):
+        if torch.is_grad_enabled():  # create_graph: a second derivative is refused, where one is asked for
+            return once_differentiable(_balance_grads)(ctx, grad_loss, grad_counts)
+        return _balance_grads(ctx, grad_loss, grad_counts)
 
 
 def balance_loss(logits: torch.Tensor, experts: Optional[torch.Tensor] = None, *, counts: Optional[torch.Tensor] = None,
@@ -82,8 +96,11 @@ def balance_loss(logits: torch.Tensor, experts: Optional[torch.Tensor] = None, *
     The gradient flows into logits through the probabilities, not through the counts.
     reduction: 'none' (per sample), 'sum' or 'mean' over the samples.
     """
-    c = lambda t: t.contiguous() if t is not None else None  # noqa: E731
-    loss, got = BalanceFunction.apply(logits.contiguous(), c(experts), c(counts), c(valid), z_weight, reduction)
+    logits = logits.contiguous()
+    experts, counts, valid = (t.contiguous() if t is not None else None for t in (experts, counts, valid))
+    desc = _lib._balance_desc(logits, experts, valid, z_weight, reduction)
+    _lib._balance_counts(logits, experts, counts)
+    loss, got = BalanceFunction.apply(logits, experts, counts, valid, desc)
     return loss, (counts if counts is not None else got)
 
 

@@ -197,6 +197,16 @@ def test_two_streams_at_once():
             assert torch.equal(r[0], want[k][0]) and torch.equal(r[1], want[k][1])
 
 
+def test_a_second_derivative_is_refused():
+    logits, ids, _ = make(0, 30, 8, 2, F32)
+    a = logits.clone().requires_grad_(True)
+    first = torch.autograd.grad(apml.balance_loss(a, ids)[0], a)[0]
+    g = torch.autograd.grad(apml.balance_loss(a, ids)[0], a, create_graph=True)[0]
+    assert torch.equal(g.detach(), first)
+    with pytest.raises(RuntimeError):
+        torch.autograd.grad(g.sum(), a)
+
+
 def test_no_tokens():
     for shape in ((0, 8), (3, 0, 8)):
         x = torch.empty(shape, device="cuda", requires_grad=True)

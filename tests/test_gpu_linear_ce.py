@@ -261,6 +261,16 @@ def test_backward_twice_and_without_gradients():
     assert apml.apml_linear_ce_forward(x, w, t, keep_state=False)[1] is None
 
 
+def test_a_second_derivative_is_refused():
+    x, w, t = make(0, 30, 40, 64, F32)
+    a = x.clone().requires_grad_(True)
+    first = torch.autograd.grad(apml.linear_ce_loss(a, w, t), a)[0]
+    g = torch.autograd.grad(apml.linear_ce_loss(a, w, t), a, create_graph=True)[0]
+    assert torch.equal(g.detach(), first)
+    with pytest.raises(RuntimeError):
+        torch.autograd.grad(g.sum(), a)
+
+
 def test_no_rows():
     for shape in ((0, 64), (3, 0, 64)):
         x = torch.empty(shape, device="cuda", dtype=BF16, requires_grad=True)
