@@ -373,8 +373,7 @@ apml_status apml_linear_ce_forward(const apml_linear_ce_desc *desc, const void *
 /*
  * Gradients of sum grad_loss * loss: grad_loss device float32 [samples][rows]
  * (NONE) or one value; x, w, target and state as in the forward call. grad_x and
- * grad_w (shapes of x and w, aligned to 16 bytes) are overwritten; one of them
- * may be NULL. The logits' gradient exists in pieces of the classes (or of the
+ * grad_w (shapes of x and w) are overwritten; one of them may be NULL. The logits' gradient exists in pieces of the classes (or of the
  * samples), rounded to x's type for the two products that read it.
  */
 apml_status apml_linear_ce_backward(const apml_linear_ce_desc *desc, const void *x, const void *w, const void *target,

@@ -658,27 +658,18 @@ template <bool PLANES> struct FinishGrad {
 };
 
 // OUT: the type of a gradient that goes out.
-template <class OUT> __device__ __forceinline__ void put(void *out, int64_t at, float v)
+template <class OUT> using Element = std::conditional_t<std::is_same_v<OUT, float>, float, uint16_t>;
+template <class OUT> __device__ __forceinline__ Element<OUT> element(float v)
 {
-    ((uint16_t *)out)[at] = OUT::from(v);
+    if constexpr (std::is_same_v<OUT, float>)
+        return v;
+    else
+        return OUT::from(v);
 }
-template <> __device__ __forceinline__ void put<float>(void *out, int64_t at, float v) { ((float *)out)[at] = v; }
-
-template <class OUT> __device__ __forceinline__ void put4(void *out, int64_t at, f32x4 v)
-{
-    *(ushort4 *)((uint16_t *)out + at) = make_ushort4(OUT::from(v[0]), OUT::from(v[1]), OUT::from(v[2]), OUT::from(v[3]));
-}
-template <class OUT> __device__ __forceinline__ void put4(void *out, int64_t at, f32x4 v, f32x4 w)
-{
-    i16x8 x;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        x[i] = (short)OUT::from(v[i]);
-        x[i + 4] = (short)OUT::from(w[i]);
-    }
-    *(i16x8 *)((uint16_t *)out + at) = x;
-}
-template <> __device__ __forceinline__ void put4<float>(void *out, int64_t at, f32x4 v) { *(f32x4 *)((float *)out + at) = v; }
+// Neighbours at any element.
+template <class T, int N> struct __attribute__((packed, aligned(sizeof(T)))) Loose {
+    T v[N];
+};
 
 // A gradient [samples][q rows][p rows]: rounded once and stored, times a factor
 // per row (coef) or for all (top).
@@ -700,20 +691,10 @@ template <class OUT> struct FinishStore {
             const int q = min(at.q0 + at.wq * (S::SQ * 16) + j * 16 + (at.lane & 15), a.q.rows - 1);
             unit[j] = (coef ? coef[(int64_t)at.sample * a.q.rows + q].unit : top->top) * inv_unit;
         }
-        constexpr int wide = std::is_same_v<OUT, float> ? 4 : 8; // 16 bytes
-        if (a.p.rows % wide == 0)
-            staged<S, wide>(a, at, unit, acc);
-        else if (a.p.rows % 4 == 0)
-            staged<S, 4>(a, at, unit, acc);
-        else
-            staged<S, 1>(a, at, unit, acc);
-    }
-    // 16 rows at a time pass through shared memory, from where a wave writes whole
-    // pieces of each row: VEC neighbours a lane.
-    template <class S, int VEC>
-    __device__ __forceinline__ void staged(const Product &a, const Place &at, const float (&unit)[S::SQ],
-                                           f32x4 (&acc)[S::SP][S::SQ]) const
-    {
+        // 16 rows at a time pass through shared memory, from where a wave writes
+        // whole pieces of each row, 16 bytes a lane wherever the row begins (a
+        // global store needs no more alignment than its elements).
+        constexpr int VEC = 16 / sizeof(Element<OUT>);
         constexpr int W = S::SP * 16, LD = W + 4; // a row of the wave's results, in float32
         static_assert(16 * LD * 4 <= S::lds / S::waves, "a wave's part of the tiles holds 16 rows");
         wait_lds_and_meet();
@@ -728,17 +709,18 @@ template <class OUT> struct FinishStore {
             const int n = min(16, a.q.rows - q0 - j * 16) * (W / VEC);
             const int64_t to = at.sample * sample + (int64_t)(q0 + j * 16) * a.p.rows + p0;
             for (int i = at.lane; i < n; i += 64) {
-                const int r = i / (W / VEC), c = i % (W / VEC) * VEC;
-                if (p0 + c >= a.p.rows)
-                    continue;
+                const int r = i / (W / VEC), c = i % (W / VEC) * VEC, left = a.p.rows - p0 - c;
                 const lds_ptr<float> from = row + r * LD + c;
-                const int64_t at_out = to + (int64_t)r * a.p.rows + c;
-                if constexpr (VEC == 8) {
-                    put4<OUT>(out, at_out, *(lds_ptr<f32x4>)from, *(lds_ptr<f32x4>)(from + 4));
-                } else if constexpr (VEC == 4) {
-                    put4<OUT>(out, at_out, *(lds_ptr<f32x4>)from);
+                auto *at_out = (Element<OUT> *)out + to + (int64_t)r * a.p.rows + c;
+                if (left >= VEC) {
+                    Loose<Element<OUT>, VEC> v;
+#pragma unroll
+                    for (int u = 0; u < VEC; ++u)
+                        v.v[u] = element<OUT>(from[u]);
+                    *(Loose<Element<OUT>, VEC> *)at_out = v;
                 } else {
-                    put<OUT>(out, at_out, *from);
+                    for (int u = 0; u < left; ++u)
+                        at_out[u] = element<OUT>(from[u]);
                 }
             }
             wave_lds();
@@ -901,11 +883,6 @@ struct Coefs {
 template <class IN> __device__ __forceinline__ float get(const void *in, int64_t at) { return IN::to(((const uint16_t *)in)[at]); }
 template <> __device__ __forceinline__ float get<float>(const void *in, int64_t at) { return ((const float *)in)[at]; }
 
-// Eight neighbours at any element.
-template <class T> struct __attribute__((packed, aligned(sizeof(T)))) Loose {
-    T v[8];
-};
-
 struct PackJob {
     const void *in;
     uint16_t *out;
@@ -967,12 +944,12 @@ template <class IN> __global__ __launch_bounds__(kBlock) void k_ce_pack(PackJobs
         // more alignment than its elements (50001 x 1003 half precision: 2.5 TB/s
         // element by element)
         if constexpr (size == 4) {
-            const Loose<float> raw = *(const Loose<float> *)((const float *)p.in + at);
+            const Loose<float, 8> raw = *(const Loose<float, 8> *)((const float *)p.in + at);
 #pragma unroll
             for (int u = 0; u < 8; ++u)
                 v[u] = raw.v[u] * f;
         } else {
-            const Loose<uint16_t> raw = *(const Loose<uint16_t> *)((const uint16_t *)p.in + at);
+            const Loose<uint16_t, 8> raw = *(const Loose<uint16_t, 8> *)((const uint16_t *)p.in + at);
 #pragma unroll
             for (int u = 0; u < 8; ++u)
                 v[u] = IN::to(raw.v[u]) * f;
@@ -1173,7 +1150,7 @@ template <class OUT> __global__ __launch_bounds__(kBlock) void k_ce_join(JoinJob
 #pragma unroll
     for (int u = 0; u < 4; ++u)
         if (c + u < jobs.cols)
-            put<OUT>(p.out, r * jobs.cols + c + u, v[u]);
+            ((Element<OUT> *)p.out)[r * jobs.cols + c + u] = element<OUT>(v[u]);
 }
 
 // ---------------------------------------------------------------------------

@@ -197,8 +197,9 @@ apml_status apml_linear_ce_backward(const apml_linear_ce_desc *desc, const void 
         return bad("state, grad_loss and one of grad_x and grad_w must be non-NULL device pointers");
     if (const apml_status st = check_inputs(*desc, x, w, target, workspace))
         return st;
-    if (!aligned(state, 16) || !aligned(grad_x, 16) || !aligned(grad_w, 16))
-        return bad("state, grad_x and grad_w must be aligned to 16 bytes");
+    const size_t size = elem_size((ElemType)desc->dtype);
+    if (!aligned(state, 16) || !aligned(grad_x, size) || !aligned(grad_w, size) || !aligned(grad_loss, 4))
+        return bad("state must be aligned to 16 bytes, the gradients to their elements");
     const CeProblem p = problem_of(*desc, x, w, target);
     const CeBackwardPlan plan = ce_plan_backward(p, grad_x, grad_w);
     if (workspace_bytes < plan.bytes)

@@ -199,6 +199,30 @@ def test_pointers_off_a_vectors_alignment(dtype, shift):
         assert torch.equal(u, v)
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+def test_gradients_off_a_vectors_alignment(dtype):
+    from paper_2512_19743_amd import _lib
+    lib = apml.load()
+    for dim in (64, 75):
+        x, w, t = make(0, 70, 300, dim, dtype)
+        one = torch.ones((), device="cuda")
+        _, state = apml.apml_linear_ce_forward(x, w, t)
+        want = apml.apml_linear_ce_backward(state, x, w, t, one)
+        d = _lib._linear_ce_desc(x, w, t, 1.0, 0.0, -100, "mean")
+        ws = _lib._ce_workspace(d, x, w, True)
+        out = [torch.full((v.numel() + 8,), 7.0, dtype=dtype, device="cuda") for v in (x, w)]
+        size = x.element_size()
+        torch.cuda.synchronize()
+        st = lib.apml_linear_ce_backward(ctypes.byref(d), x.data_ptr(), w.data_ptr(), t.data_ptr(), state.data_ptr(),
+                                         one.data_ptr(), out[0].data_ptr() + 3 * size, out[1].data_ptr() + size,
+                                         ws.data_ptr(), ws.numel(), None)
+        torch.cuda.synchronize()
+        assert st == 0
+        for o, at, v in zip(out, (3, 1), want):
+            assert torch.equal(o[at:at + v.numel()].view_as(v), v)
+            assert (o[:at] == 7.0).all() and (o[at + v.numel():] == 7.0).all()
+
+
 def test_strided_inputs():
     x, w, t = make(0, 70, 300, 64, BF16)
     xs = torch.stack([x, x], 1)[:, 0]
