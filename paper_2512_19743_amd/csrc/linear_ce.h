@@ -39,6 +39,7 @@ struct CeProblem {
 // pointers' alignment alone.
 struct CeForwardPlan {
     bool pack_x, pack_w;         // copied: rows of dim_pad elements, in planes for float32
+    bool whole_f32;              // float32 multiplied as it is
     int dim_pad;                 // dim up to a multiple of kCeStep
     int parts;                   // groups of classes with a maximum and a sum of their own
     size_t x, w, part, picked, sums, ticket, bytes;

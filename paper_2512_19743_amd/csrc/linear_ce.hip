@@ -81,6 +81,19 @@ struct F16 {
     }
 };
 
+// float32 as it is, two 16-bit elements a value: a fragment's 16 bytes are four
+// neighbours, one for each of four instructions, on either side alike.
+struct F32 {
+    static __device__ __forceinline__ f32x4 mma(i16x8 a, i16x8 b, f32x4 c)
+    {
+        const f32x4 x = __builtin_bit_cast(f32x4, a), y = __builtin_bit_cast(f32x4, b);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            c = __builtin_amdgcn_mfma_f32_16x16x4f32(x[i], y[i], c, 0, 0, 0);
+        return c;
+    }
+};
+
 // v cut into three bfloat16 values of 8 significant bits: v = a + b + c exactly
 // (truncated, so that no finite value becomes infinite).
 struct Planes {
@@ -135,7 +148,7 @@ template <int ROWS> __device__ __forceinline__ int k_swizzle(int k)
 // `j` (1 KB of the tile) fetches. With k contiguous the tile holds ROWS rows of
 // 8 chunks of 16 bytes, chunk c of row r in slot c ^ (r & 7): the 16 rows that a
 // fragment read touches then lie in different banks (EIGHTS: the rows that
-// p_fragment touches). With the rows contiguous it holds kCeStep rows of ROWS / 8
+// such a fragment touches). With the rows contiguous it holds kCeStep rows of ROWS / 8
 // chunks, moved by k_swizzle for the same reason (a transposing read touches the
 // same columns of 16 rows).
 // The base is that of row first_row (a tile of the padded rows may begin behind
@@ -1181,8 +1194,9 @@ bool large_tiles(int64_t p, int64_t q, int64_t batches)
 }
 
 // The tile of a product of p classes and q rows, `batches` of them. Forward, 16
-// rows where there are no more (one row of 131072 x 4096: w streams at 6 TB/s);
-// backward the logits' gradient is written for whole steps of rows.
+// rows where there are no more (one row of 131072 x 4096 195 us, of 32000 x 4096
+// 46; in tiles of 128 206 and 65); backward the logits' gradient is written for
+// whole steps of rows.
 Kind choose(int64_t p, int64_t q, int64_t batches, bool forward)
 {
     if (forward && q <= 16)
@@ -1276,6 +1290,15 @@ void choose_packs(const CeProblem &p, bool *x, bool *w)
     *w = p.type == ElemType::f32 || p.dim % 8 || !aligned16(p.w);
 }
 
+// Whether a forward pass in float32 multiplies x and w as they are: where the rows
+// are one tile it is bound by w, which is then read once instead of copied into
+// planes that are read (one row of 131072 x 4096: 396 us, by planes 2084; 128 rows
+// 977 and 2038); with more rows the planes' products are the faster ones.
+bool whole_float32(const CeProblem &p)
+{
+    return p.type == ElemType::f32 && p.rows <= 128 && p.dim % (kCeStep / 2) == 0 && aligned16(p.x) && aligned16(p.w);
+}
+
 // The copies that a pass needs, in one launch.
 struct Packs {
     PackJobs jobs{};
@@ -1360,9 +1383,11 @@ static int row_threads(int64_t n) { return n >= 32768 ? 4 : n >= 256 ? 16 : kBlo
 CeForwardPlan ce_plan_forward(const CeProblem &p)
 {
     CeForwardPlan f{};
-    choose_packs(p, &f.pack_x, &f.pack_w);
+    f.whole_f32 = whole_float32(p);
+    if (!f.whole_f32)
+        choose_packs(p, &f.pack_x, &f.pack_w);
     f.dim_pad = (int)pad_to(p.dim, kCeStep);
-    const Kind kind = choose(p.classes, p.rows, p.samples, true);
+    const Kind kind = f.whole_f32 && p.rows > 16 ? Kind::medium : choose(p.classes, p.rows, p.samples, true);
     f.parts = ceil_to(p.classes, tile_p(kind)) * waves_p(kind);
     const int64_t n = all_rows(p);
     Offsets o;
@@ -1386,7 +1411,24 @@ void ce_forward(const CeProblem &p, const CeForwardPlan &plan, uint8_t *ws, floa
     auto *ticket = (int *)(ws + plan.ticket);
     const Targets target = targets_of(p);
     auto *x = (uint16_t *)(ws + plan.x), *w = (uint16_t *)(ws + plan.w);
-    by_type(p.type, [&](auto elem, auto cut, auto io) {
+    const FinishStats finish{target, part, picked, ticket, scale2_of(p)};
+    if (plan.whole_f32) {
+        Product a{};
+        a.p = features(p, false, p.w, nullptr, p.classes, 0);
+        a.q = features(p, false, p.x, nullptr, p.rows, 0);
+        for (Operand *o : {&a.p, &a.q}) { // in 16-bit elements
+            o->ld *= 2;
+            o->sample *= 2;
+            o->k *= 2;
+        }
+        a.steps = a.p.k / kCeStep;
+        a.samples = p.samples;
+        a.splits = 1;
+        if (p.rows <= 16)
+            launch_shape<F32, false, false, false, Narrow>(a, p.classes, p.rows, finish, s);
+        else
+            launch_shape<F32, false, false, false, Medium>(a, p.classes, p.rows, finish, s);
+    } else by_type(p.type, [&](auto elem, auto cut, auto io) {
         using ELEM = decltype(elem);
         using IO = decltype(io);
         Packs packs;
@@ -1404,8 +1446,7 @@ void ce_forward(const CeProblem &p, const CeForwardPlan &plan, uint8_t *ws, floa
         a.samples = p.samples;
         a.splits = 1;
         launch_product<ELEM, decltype(cut)::value, false, false>(choose(p.classes, p.rows, p.samples, true), a,
-                                                                 p.classes, p.rows,
-                                                                 FinishStats{target, part, picked, ticket, scale2_of(p)}, s);
+                                                                 p.classes, p.rows, finish, s);
     });
     const auto join = [&](auto threads) {
         constexpr int T = decltype(threads)::value;
