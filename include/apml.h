@@ -314,7 +314,8 @@ const char *apml_phase_name(int32_t phase);
  * to 256 bytes, free for other use once the call's kernels have run; two calls
  * that may overlap need two), and what the backward pass needs of the forward
  * one lies in a state array of the caller's. So every call can be captured into
- * a graph. Gradients are overwritten. All sums are held in float32 or more.
+ * a graph (after one of its kind outside: the runtime loads a kernel with its
+ * first launch). Gradients are overwritten. All sums are held in float32 or more.
  */
 typedef enum { APML_F32 = 0, APML_BF16 = 1, APML_F16 = 2 } apml_dtype;
 typedef enum { APML_I64 = 0, APML_I32 = 1 } apml_index_type;

@@ -483,8 +483,8 @@ def _linear_ce_desc(x, w, target, scale, z_weight, ignore_index, reduction) -> a
     samples = ws[0] if len(ws) == 3 else 1
     # no row: the caller launches nothing
     rows = target.numel() // samples if samples else 0
-    if max(samples, rows, ws[-2], xs[-1]) >= 1 << 31:
-        raise ValueError("a size is beyond the library's 32-bit range")
+    if max(samples, rows, ws[-2], xs[-1]) >= 1 << 31 or not -(1 << 63) <= ignore_index < 1 << 63:
+        raise ValueError("a size or ignore_index is beyond the library's range")
     return apml_linear_ce_desc(ctypes.sizeof(apml_linear_ce_desc), _DTYPES[x.dtype], _INDEX_TYPES[target.dtype], samples,
                                rows, ws[-2], xs[-1], _REDUCTIONS[reduction], scale, z_weight, ignore_index)
 

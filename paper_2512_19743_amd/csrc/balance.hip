@@ -97,7 +97,8 @@ __device__ __forceinline__ void load_row(const typename L::raw *row, int lane, i
 
 // Rows that cannot be read 16 bytes at a time pass through shared memory: their
 // tokens lie one after another, so a tile of them is read in whole 16-byte words
-// wherever it starts (161 experts in half precision: element by element 1.4 TB/s).
+// wherever it starts (13 x 7001 tokens of 161 experts in half precision, backward:
+// 31 us, element by element 42).
 // An element keeps its place within its word; returns the first one's.
 template <class R> __device__ __forceinline__ R *tile_in(R *lds, const R *src, int n)
 {
@@ -189,6 +190,9 @@ struct BalanceArgs {
     int *ticket;   // cleared for k_balance_join
 };
 
+// A chunk's sums of the probabilities, its tokens per expert and its sum of lse^2.
+// Bound by the latency of few rows a lane group (16 x 8192 tokens of 64 experts in
+// bfloat16, 17 MB: 14 us) and, for rows of odd length, by the exponentials.
 template <class L, int VEC, int NV>
 __global__ __launch_bounds__(kBlock) void k_balance_chunks(BalanceArgs a, bool index32)
 {
@@ -306,7 +310,8 @@ struct Share {
     int count;
 };
 
-// Joins a sample's chunks: one workgroup a sample.
+// Joins a sample's chunks in double precision: one workgroup a sample (128 chunks
+// of 64 experts: 7 us, a chain of a few loads and barriers).
 __global__ __launch_bounds__(1024) void k_balance_join(BalanceArgs a, int64_t *counts, float *loss, float *state,
                                                        int reduction, float *per, int *ticket)
 {
@@ -412,6 +417,8 @@ __global__ __launch_bounds__(1024) void k_balance_join(BalanceArgs a, int64_t *c
         loss[0] = (float)(reduction == 2 ? v / (double)gridDim.x : v);
 }
 
+// The logits' gradient, with the softmax computed again (16 x 8192 x 64 bfloat16,
+// 34 MB read and written: 13 us).
 template <class L, int VEC, int NV>
 __global__ __launch_bounds__(kBlock) void k_balance_grad(BalanceArgs a, const float *state, const float *grad_loss,
                                                          int per_sample, float factor, void *out)
@@ -466,7 +473,8 @@ __global__ __launch_bounds__(kBlock) void k_balance_grad(BalanceArgs a, const fl
             finish(v, vr, (typename L::raw *)out + r * a.E);
             if (two)
                 finish(w, vq, (typename L::raw *)out + q * a.E);
-        }    } else {
+        }
+    } else {
         extern __shared__ __attribute__((aligned(16))) float sm[];
         using R = typename L::raw;
         R *lds = (R *)sm;
@@ -494,7 +502,8 @@ __global__ __launch_bounds__(kBlock) void k_counts_clear(unsigned long long *cou
         counts[i] = 0;
 }
 
-// Integer sums: the order of the atomics does not show.
+// Integer sums: the order of the atomics does not show. Bound by the read of the
+// indices (16.8 million int64, 134 MB: 29 us, 4.6 TB/s).
 template <bool I32>
 __global__ __launch_bounds__(kBlock) void k_counts(BalanceArgs a, unsigned long long *counts)
 {

@@ -490,6 +490,8 @@ def test_binding_refuses():
     with pytest.raises(ValueError):
         apml.linear_ce_loss(x, w, t, reduction="average")
     with pytest.raises(ValueError):
+        apml.linear_ce_loss(x, w, t, ignore_index=2 ** 64 - 100)
+    with pytest.raises(ValueError):
         apml.apml_linear_ce_forward(x.t(), w, t)
     with pytest.raises(apml.ApmlError):
         apml.linear_ce_loss(x, w, t, scale=float("nan"))
