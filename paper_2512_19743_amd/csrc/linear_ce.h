@@ -54,7 +54,7 @@ struct CeBackwardPlan {
     bool pack_x, pack_w;
     int dim_pad, rows_pad;       // rows up to a multiple of kCeStep
     int piece_samples, piece_classes; // the part of the logits' gradient that exists at a time
-    int ld_g;                    // its columns, a multiple of kCeStep
+    int ld_g;                    // elements of a row of it, a multiple of kCeStep
     int split_x, split_w;        // parts of the sum over the classes (grad_x) and over the rows (grad_w)
     bool sum_x;                  // grad_x is summed in float32 over several pieces or parts
     int tops;                    // workgroups of the pass over the upstream gradients (0: all rows have the same)
