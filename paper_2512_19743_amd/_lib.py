@@ -70,6 +70,14 @@ class apml_memory_stats(ctypes.Structure):
     _fields_ = [("in_use", ctypes.c_int64), ("peak_in_use", ctypes.c_int64), ("reserved", ctypes.c_int64)]
 
 
+try:  # the current stream's handle without a Stream object around it (8 us of a small call)
+    from torch._C import _cuda_getCurrentRawStream as _raw_stream, _cuda_getDevice as _current_device
+except ImportError:
+    _current_device = torch.cuda.current_device
+
+    def _raw_stream(device: int) -> int:
+        return torch.cuda.current_stream(device).cuda_stream
+
 ALLOC_FN = ctypes.CFUNCTYPE(ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p, ctypes.c_void_p)
 FREE_FN = ctypes.CFUNCTYPE(None, ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p, ctypes.c_void_p)
 
@@ -394,6 +402,7 @@ def apml_dense_backward(plan: DensePlan, x: torch.Tensor, y: torch.Tensor, grad_
 _DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 _INDEX_TYPES = {torch.int64: 0, torch.int32: 1}
 _REDUCTIONS = {"none": 0, "sum": 1, "mean": 2}
+_CE_DESC_SIZE, _BALANCE_DESC_SIZE = ctypes.sizeof(apml_linear_ce_desc), ctypes.sizeof(apml_balance_desc)
 
 
 def _on_gpu(name: str, t: torch.Tensor, types, device: Optional[int] = None) -> int:
@@ -425,13 +434,13 @@ class _Queued:
             if stream.device != like.device:
                 raise ValueError(f"stream must be on {like.device}, got {stream.device}")
             self.guard = torch.cuda.stream(stream)
-        elif torch.cuda.current_device() != self.device:
+        elif _current_device() != self.device:  # a tensor is there: the runtime is initialised
             self.guard = torch.cuda.device(self.device)
 
     def __enter__(self):
         if self.guard is not None:
             self.guard.__enter__()
-        return self.stream.cuda_stream if self.stream is not None else torch.cuda.current_stream(self.device).cuda_stream
+        return self.stream.cuda_stream if self.stream is not None else _raw_stream(self.device)
 
     def __exit__(self, *exc):
         if self.guard is not None:
@@ -485,7 +494,7 @@ def _linear_ce_desc(x, w, target, scale, z_weight, ignore_index, reduction) -> a
     rows = target.numel() // samples if samples else 0
     if max(samples, rows, ws[-2], xs[-1]) >= 1 << 31 or not -(1 << 63) <= ignore_index < 1 << 63:
         raise ValueError("a size or ignore_index is beyond the library's range")
-    return apml_linear_ce_desc(ctypes.sizeof(apml_linear_ce_desc), _DTYPES[x.dtype], _INDEX_TYPES[target.dtype], samples,
+    return apml_linear_ce_desc(_CE_DESC_SIZE, _DTYPES[x.dtype], _INDEX_TYPES[target.dtype], samples,
                                rows, ws[-2], xs[-1], _REDUCTIONS[reduction], scale, z_weight, ignore_index)
 
 
@@ -580,7 +589,7 @@ def _balance_desc(logits, index, valid, z_weight, reduction) -> apml_balance_des
         raise ValueError("need at least one sample and one expert")
     if max(samples, tokens, experts, chosen) >= 1 << 31:
         raise ValueError("a size is beyond the library's 32-bit range")
-    return apml_balance_desc(ctypes.sizeof(apml_balance_desc), _DTYPES[logits.dtype], _INDEX_TYPES[index_type], samples,
+    return apml_balance_desc(_BALANCE_DESC_SIZE, _DTYPES[logits.dtype], _INDEX_TYPES[index_type], samples,
                              tokens, experts, chosen, _REDUCTIONS[reduction], z_weight)
 
 
