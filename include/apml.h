@@ -343,7 +343,7 @@ typedef struct apml_linear_ce_desc {
     int32_t samples;      /* >= 1 */
     int32_t rows;         /* >= 1, per sample; samples * rows <= 2^26 */
     int32_t classes;      /* >= 1, <= 2^26 */
-    int32_t dim;          /* >= 1, <= 2^20 */
+    int32_t dim;          /* >= 1, <= 2^20; some 2^38 logits, or 2^35 features of either side, a call */
     int32_t reduction;    /* apml_reduction */
     float scale;          /* 1 / temperature */
     float z_weight;       /* weight of lse^2 */
@@ -374,8 +374,9 @@ apml_status apml_linear_ce_forward(const apml_linear_ce_desc *desc, const void *
 /*
  * Gradients of sum grad_loss * loss: grad_loss device float32 [samples][rows]
  * (NONE) or one value; x, w, target and state as in the forward call. grad_x and
- * grad_w (shapes of x and w) are overwritten; one of them may be NULL. The logits' gradient exists in pieces of the classes (or of the
- * samples), rounded to x's type for the two products that read it.
+ * grad_w (shapes of x and w) are overwritten; one of them may be NULL. The logits'
+ * gradient exists in pieces of the classes (or of the samples), rounded to x's
+ * type for the two products that read it.
  */
 apml_status apml_linear_ce_backward(const apml_linear_ce_desc *desc, const void *x, const void *w, const void *target,
                                     const float *state, const float *grad_loss, void *grad_x, void *grad_w,

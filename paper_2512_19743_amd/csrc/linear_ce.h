@@ -16,11 +16,10 @@ inline size_t elem_size(ElemType t) { return t == ElemType::f32 ? 4 : 2; }
 constexpr int kCeStep = 64; // elements of the summed axis that one step of a product takes
 
 // What the forward pass keeps of a row: its largest logit in units of log 2,
-// 1 / sum exp(z - top),
-// the part of its softmax that is not the target's, and its
-// log-sum-exp. The loss and the target's gradient come from `miss`, a sum without the target's
-// term: where the target's probability is next to 1, lse - z_target and p - 1
-// would be differences of nearly equal numbers.
+// 1 / sum exp(z - top), the part of its softmax that is not the target's, and its
+// log-sum-exp. The loss and the target's gradient come from `miss`, a sum without
+// the target's term: where the target's probability is next to 1, lse - z_target
+// and p - 1 would be differences of nearly equal numbers.
 struct CeRow {
     float top, inv_total, miss, lse;
 };
@@ -45,6 +44,9 @@ struct CeForwardPlan {
     size_t x, w, part, picked, sums, ticket, bytes;
 };
 CeForwardPlan ce_plan_forward(const CeProblem &p);
+// Whether every launch of the two passes has fewer than 2^32 threads, which is
+// what a dispatch counts them in.
+bool ce_launches_fit(const CeProblem &p);
 // loss: [samples * rows] (reduction none) or [1]; rows: the state or NULL;
 // total: two floats (sum of the losses, rows that count) or NULL.
 void ce_forward(const CeProblem &p, const CeForwardPlan &plan, uint8_t *ws, float *loss, CeRow *rows, float *total,

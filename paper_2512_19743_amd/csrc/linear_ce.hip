@@ -898,8 +898,9 @@ struct Coefs {
 };
 
 // Rows copied to dim_pad columns (zeros behind dim) and, where scaled, rows_out
-// rows a sample with every row times its unit over the largest one (a power of
-// two, so no rounding; zero for ignored rows, whatever they hold). In the backward
+// rows a sample with every row times its unit over the largest one (a power of two:
+// no rounding but of float16 values below its normal range, an absolute step of
+// 2^-25 of the largest row's; zero for ignored rows, whatever they hold). In the backward
 // pass the first coef_blocks workgroups write the rows' coefficients. Bound by
 // memory (50001 x 1003 to 50001 x 1024 half precision, 203 MB: 45 us, 4.5 TB/s).
 template <class IN> __device__ __forceinline__ float get(const void *in, int64_t at) { return IN::to(((const uint16_t *)in)[at]); }
@@ -1384,6 +1385,23 @@ template <class F> void by_type(ElemType t, F f)
 }
 
 } // namespace
+
+// The products in tiles of 128 x 128, 256 threads each: larger ones have half as
+// many a result or fewer, those of 16 rows stand where there are no more, and a sum
+// is cut into parts only where its tiles are few. The logits' gradient is cut into
+// pieces far below the limit.
+bool ce_launches_fit(const CeProblem &p)
+{
+    constexpr int64_t limit = ((int64_t)1 << 32) - 8 * kBlock; // every job of a launch ends in whole workgroups
+    const int64_t rows = (int64_t)ceil_to(p.rows, 128) * p.samples, classes = (int64_t)ceil_to(p.classes, 128) * p.samples;
+    const int64_t features = ceil_to(p.dim, 128), dim_pad = pad_to(p.dim, kCeStep);
+    bool x, w;
+    choose_packs(p, &x, &w);
+    const int64_t copied = (x ? all_rows(p) : 0) + (w ? (int64_t)p.samples * p.classes : 0) +
+                           p.samples * pad_to(p.rows, kCeStep);
+    return rows * ceil_to(p.classes, 128) * 256 < limit && std::max(rows, classes) * features * 256 < limit &&
+           copied * dim_pad / 8 + all_rows(p) < limit && p.rows * pad_to(p.dim, 4) / 4 < limit;
+}
 
 // Threads of k_ce_rows a row: with few rows, as many as it takes to have the
 // parts' loads in flight together (one row of 131072 classes, 4096 parts: 16

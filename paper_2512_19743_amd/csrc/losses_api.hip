@@ -49,11 +49,14 @@ apml_status check_desc(const apml_linear_ce_desc *d)
     // a launch's workgroups and the offsets within a tile are 32-bit
     if (d->dim > (1 << 20) || d->classes > (1 << 26) || (int64_t)d->samples * d->rows > (1 << 26))
         return fail_with(APML_ERR_UNSUPPORTED, "dim beyond 2^20, classes beyond 2^26 or samples * rows beyond 2^26");
-    if ((((int64_t)d->classes + 127) / 128 + ((int64_t)d->dim + 127) / 128) * (((int64_t)d->rows + 15) / 16) *
-            d->samples > ((int64_t)1 << 30) ||
-        (((int64_t)d->classes + 127) / 128) * (((int64_t)d->dim + 127) / 128) * d->samples > ((int64_t)1 << 24))
-        return fail_with(APML_ERR_UNSUPPORTED, "too many tiles for one launch");
+    if ((((int64_t)d->classes + 127) / 128) * (((int64_t)d->dim + 127) / 128) * d->samples > ((int64_t)1 << 24))
+        return fail_with(APML_ERR_UNSUPPORTED, "too many classes and features for one launch");
     return APML_OK;
+}
+
+apml_status check_launches(const CeProblem &p)
+{
+    return ce_launches_fit(p) ? APML_OK : fail_with(APML_ERR_UNSUPPORTED, "too many rows, classes or features for one launch");
 }
 
 CeProblem problem_of(const apml_linear_ce_desc &d, const void *x, const void *w, const void *target)
@@ -156,6 +159,8 @@ apml_status apml_linear_ce_workspace(const apml_linear_ce_desc *desc, const void
     if (!forward_bytes && !backward_bytes)
         return bad("forward_bytes or backward_bytes must be non-NULL");
     const CeProblem p = problem_of(*desc, x ? x : kUnaligned, w ? w : kUnaligned, nullptr);
+    if (const apml_status st = check_launches(p))
+        return st;
     if (forward_bytes)
         *forward_bytes = ce_plan_forward(p).bytes;
     if (backward_bytes)
@@ -174,9 +179,11 @@ apml_status apml_linear_ce_forward(const apml_linear_ce_desc *desc, const void *
         return bad("loss must be a non-NULL device pointer");
     if (const apml_status st = check_inputs(*desc, x, w, target, workspace))
         return st;
-    if (!aligned(state, 16))
-        return bad("state must be aligned to 16 bytes");
+    if (!aligned(loss, 4) || !aligned(state, 16))
+        return bad("loss must be aligned to 4 bytes, state to 16");
     const CeProblem p = problem_of(*desc, x, w, target);
+    if (const apml_status st = check_launches(p))
+        return st;
     const CeForwardPlan plan = ce_plan_forward(p);
     if (workspace_bytes < plan.bytes)
         return short_workspace("apml_linear_ce_forward", plan.bytes, workspace_bytes);
@@ -201,6 +208,8 @@ apml_status apml_linear_ce_backward(const apml_linear_ce_desc *desc, const void 
     if (!aligned(state, 16) || !aligned(grad_x, size) || !aligned(grad_w, size) || !aligned(grad_loss, 4))
         return bad("state must be aligned to 16 bytes, the gradients to their elements");
     const CeProblem p = problem_of(*desc, x, w, target);
+    if (const apml_status st = check_launches(p))
+        return st;
     const CeBackwardPlan plan = ce_plan_backward(p, grad_x, grad_w);
     if (workspace_bytes < plan.bytes)
         return short_workspace("apml_linear_ce_backward", plan.bytes, workspace_bytes);
@@ -240,6 +249,8 @@ apml_status apml_balance_forward(const apml_balance_desc *desc, const void *logi
         return bad("logits, counts, loss and workspace must be non-NULL device pointers");
     if (!aligned(logits, elem_size((ElemType)desc->dtype)) || !aligned(index, desc->index_type == APML_I32 ? 4 : 8))
         return bad("logits and index must be aligned to their elements");
+    if (!aligned(counts, 8) || !aligned(loss, 4) || !aligned(state, 4))
+        return bad("counts, loss and state must be aligned to their elements");
     if (!aligned(workspace, 256))
         return bad("workspace must be aligned to 256 bytes");
     const BalanceProblem p = problem_of(*desc, logits, index, valid);
@@ -259,8 +270,8 @@ apml_status apml_balance_backward(const apml_balance_desc *desc, const void *log
     if (!logits || !state || !grad_loss || !grad_logits)
         return bad("logits, state, grad_loss and grad_logits must be non-NULL device pointers");
     const size_t size = elem_size((ElemType)desc->dtype);
-    if (!aligned(logits, size) || !aligned(grad_logits, size))
-        return bad("logits and grad_logits must be aligned to their elements");
+    if (!aligned(logits, size) || !aligned(grad_logits, size) || !aligned(state, 4) || !aligned(grad_loss, 4))
+        return bad("logits, grad_logits, state and grad_loss must be aligned to their elements");
     balance_backward(problem_of(*desc, logits, nullptr, valid), state, grad_loss, grad_logits, (hipStream_t)stream);
     return launched();
 }
@@ -280,8 +291,8 @@ apml_status apml_expert_counts(const void *index, int32_t index_type, const uint
         return st;
     if (!index || !counts)
         return bad("index and counts must be non-NULL device pointers");
-    if (!aligned(index, index_type == APML_I32 ? 4 : 8))
-        return bad("index must be aligned to its elements");
+    if (!aligned(index, index_type == APML_I32 ? 4 : 8) || !aligned(counts, 8))
+        return bad("index and counts must be aligned to their elements");
     expert_counts(problem_of(d, nullptr, index, valid), counts, (hipStream_t)stream);
     return launched();
 }

@@ -125,3 +125,37 @@ def test_binding_refuses_cpu_tensors():
         apml.balance_loss(x, t.unsqueeze(1))
     with pytest.raises(ValueError, match="GPU"):
         apml.expert_counts(t.unsqueeze(1), 8)
+
+
+# a dispatch counts its threads in 32 bits
+MANY = [dict(rows=1 << 20, classes=1 << 18, dim=64), dict(rows=1 << 26, classes=1 << 12, dim=64),
+        dict(samples=1 << 15, rows=1 << 11, classes=1 << 13, dim=64), dict(rows=1 << 20, classes=256, dim=(1 << 15) + 1),
+        dict(rows=16, classes=1 << 25, dim=1025), dict(rows=64, classes=1 << 26, dim=4096)]
+
+
+@pytest.mark.parametrize("kw", MANY)
+@pytest.mark.parametrize("dtype", [0, 1, 2])
+def test_linear_ce_refuses_launches_of_too_many_threads(kw, dtype):
+    lib, d, n = _lib.load(), ce_desc(dtype=dtype, **kw), ctypes.c_size_t()
+    big = 1 << 62
+    assert lib.apml_linear_ce_workspace(ctypes.byref(d), None, None, ctypes.byref(n), ctypes.byref(n)) == 2
+    assert lib.apml_linear_ce_forward(ctypes.byref(d), FAKE, FAKE, FAKE, FAKE, FAKE, FAKE, big, None) == 2
+    assert lib.apml_linear_ce_backward(ctypes.byref(d), FAKE, FAKE, FAKE, FAKE, FAKE, FAKE, FAKE, FAKE, big, None) == 2
+
+
+@pytest.mark.parametrize("kw", [dict(rows=1 << 20, classes=1 << 17, dim=4096), dict(rows=1 << 26, classes=1000, dim=64),
+                                dict(rows=1, classes=1 << 26, dim=512), dict(samples=1 << 20, rows=64, classes=64, dim=64)])
+def test_large_calls_are_taken(kw):
+    lib, d, n = _lib.load(), ce_desc(dtype=1, **kw), ctypes.c_size_t()
+    assert lib.apml_linear_ce_workspace(ctypes.byref(d), FAKE, FAKE, ctypes.byref(n), ctypes.byref(n)) == 0 and n.value > 0
+
+
+def test_results_off_their_elements_are_refused():
+    lib, d, b = _lib.load(), ce_desc(), balance_desc()
+    big = 1 << 60
+    assert lib.apml_linear_ce_forward(ctypes.byref(d), FAKE, FAKE, FAKE, ODD, FAKE, FAKE, big, None) == 1
+    for counts, loss, state in ((ctypes.c_void_p(FAKE.value + 4), FAKE, FAKE), (FAKE, ODD, FAKE), (FAKE, FAKE, ODD)):
+        assert lib.apml_balance_forward(ctypes.byref(b), FAKE, FAKE, None, counts, loss, state, FAKE, big, None) == 1
+    for state, g in ((ODD, FAKE), (FAKE, ODD)):
+        assert lib.apml_balance_backward(ctypes.byref(b), FAKE, None, state, g, FAKE, None) == 1
+    assert lib.apml_expert_counts(FAKE, 0, None, 1, 8, 2, 4, ctypes.c_void_p(FAKE.value + 4), None) == 1
