@@ -494,6 +494,8 @@ def _linear_ce_desc(x, w, target, scale, z_weight, ignore_index, reduction) -> a
     rows = target.numel() // samples if samples else 0
     if max(samples, rows, ws[-2], xs[-1]) >= 1 << 31 or not -(1 << 63) <= ignore_index < 1 << 63:
         raise ValueError("a size or ignore_index is beyond the library's range")
+    if isinstance(scale, torch.Tensor) or isinstance(z_weight, torch.Tensor):  # would go without its gradient
+        raise ValueError("scale and z_weight must be numbers (a learned scale is multiplied into x)")
     return apml_linear_ce_desc(_CE_DESC_SIZE, _DTYPES[x.dtype], _INDEX_TYPES[target.dtype], samples,
                                rows, ws[-2], xs[-1], _REDUCTIONS[reduction], scale, z_weight, ignore_index)
 
@@ -589,6 +591,8 @@ def _balance_desc(logits, index, valid, z_weight, reduction) -> apml_balance_des
         raise ValueError("need at least one sample and one expert")
     if max(samples, tokens, experts, chosen) >= 1 << 31:
         raise ValueError("a size is beyond the library's 32-bit range")
+    if isinstance(z_weight, torch.Tensor):  # would go without its gradient
+        raise ValueError("z_weight must be a number")
     return apml_balance_desc(_BALANCE_DESC_SIZE, _DTYPES[logits.dtype], _INDEX_TYPES[index_type], samples,
                              tokens, experts, chosen, _REDUCTIONS[reduction], z_weight)
 

@@ -46,7 +46,8 @@ def linear_ce_loss(x: torch.Tensor, w: torch.Tensor, target: torch.Tensor, *, sc
 
     x (..., dim) and w (classes, dim): one set of classes, a code book or a vocabulary. x (B, N, dim) and
     w (B, M, dim): each sample with its own, as when the descriptors of one cloud's points are matched to
-    those of the other's (scale: 1 / temperature). float32, bfloat16 or float16 GPU tensors.
+    those of the other's (scale, a number: 1 / temperature; a learned one is multiplied into x).
+    float32, bfloat16 or float16 GPU tensors.
     target: the rows' classes, int64 or int32, of x's leading shape; ignore_index: a row that adds nothing.
     z_weight: weight of the squared log-sum-exp that is added per row.
     reduction: 'none' (target's shape), 'sum', or 'mean' over the rows that are not ignored.

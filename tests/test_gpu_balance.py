@@ -318,3 +318,15 @@ def test_a_training_step_of_all_losses_together():
     near(got[4], 0.01 * gr)
     r = oracle.linear_ce(feats.detach(), feats_ref.detach(), match, scale=0.3)
     oracle.within(gm[0], r["grad_x"], r["grad_x_tol"], "descriptors")
+
+
+@pytest.mark.parametrize("mode", [torch.no_grad, torch.inference_mode])
+def test_measured_without_gradients(mode):
+    logits, ids, valid = make(2, 100, 16, 2, BF16, padded=0.2)
+    want, tokens = apml.balance_loss(logits, ids, valid=valid)
+    with mode():
+        got, count = apml.balance_loss(logits, ids, valid=valid)
+        again, _ = apml.balance_loss(logits, counts=count, valid=valid)
+    assert torch.equal(got, want) and torch.equal(again, want) and torch.equal(count, tokens)
+    with pytest.raises(ValueError, match="number"):
+        apml.balance_loss(logits, ids, valid=valid, z_weight=torch.zeros(()))

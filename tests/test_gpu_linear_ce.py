@@ -500,3 +500,28 @@ def test_binding_refuses():
         apml.apml_linear_ce_backward(state[:5].contiguous(), x, w, t, torch.ones((), device="cuda"))
     with pytest.raises(ValueError):
         apml.apml_linear_ce_backward(state, x, w, t, torch.ones(20, device="cuda"))
+
+
+def test_a_scale_that_is_a_tensor_is_refused():
+    """It would be read without its gradient."""
+    x, w, t = make(0, 20, 30, 64, BF16)
+    for kw in (dict(scale=torch.ones((), requires_grad=True)), dict(z_weight=torch.zeros(()))):
+        with pytest.raises(ValueError, match="number"):
+            apml.linear_ce_loss(x, w, t, **kw)
+    learned = torch.tensor(1.5, device="cuda", requires_grad=True)
+    xf, wf = x.float(), w.float()
+    apml.linear_ce_loss(xf * learned, wf, t).backward()
+    want = torch.tensor(1.5, dtype=torch.float64, requires_grad=True)
+    torch.nn.functional.cross_entropy((xf.cpu().double() * want) @ wf.cpu().double().T, t.cpu()).backward()
+    # a sum of rows * dim terms in float32, each off by 2^-16 at most
+    size = (xf.abs().double().sum() * wf.abs().double().amax()).item()
+    assert abs(learned.grad.item() - want.grad.item()) <= 2.0 ** -16 * size
+
+
+@pytest.mark.parametrize("mode", [torch.no_grad, torch.inference_mode])
+def test_scored_without_gradients(mode):
+    x, w, t = make(0, 20, 300, 64, BF16)
+    want = apml.linear_ce_loss(x, w, t, reduction="none")
+    with mode():
+        got = apml.linear_ce_loss(x, w.requires_grad_(), t, reduction="none")
+    assert torch.equal(got, want) and not got.requires_grad
