@@ -272,7 +272,7 @@ struct Place {
 // step, and keeps the matrix cores 60 to 65% busy at 2.0 to 2.25 GHz (power sets
 // the clock): 1.28 to 1.43 PFLOP/s at 8192 x 131072 x 4096 and its gradients.
 template <class ELEM, bool PLANES, bool PK, bool QK, class S, class Finish>
-__global__ __launch_bounds__(S::threads) void k_product(Product a, Finish finish)
+__device__ __forceinline__ void product(const Product &a, const Finish &finish, int block, int blocks)
 {
     extern __shared__ __attribute__((aligned(1024))) char smem[];
     const int lane = lane_id();
@@ -286,7 +286,7 @@ __global__ __launch_bounds__(S::threads) void k_product(Product a, Finish finish
         // The workgroups of an XCD take a run of tiles; within it, `group` q
         // tiles for one p tile after the other, so that the tiles in flight
         // share rows of both operands in that XCD's L2.
-        int id = xcd_contiguous((int)blockIdx.x, (int)gridDim.x);
+        int id = xcd_contiguous(block, blocks);
         const int per = a.tiles_p * a.tiles_q;
         at.split = id % a.splits;
         id /= a.splits;
@@ -458,6 +458,12 @@ __global__ __launch_bounds__(S::threads) void k_product(Product a, Finish finish
     // lane l holds, of 16 x 16 results, q = l & 15 and p = 4 (l >> 4) .. + 3; with
     // P's k contiguous, of 32 x 16, p = 8 (l >> 4) .. + 7 in two neighbours acc
     finish.template operator()<ELEM, S>(a, at, rows, acc);
+}
+
+template <class ELEM, bool PLANES, class S, class Finish>
+__global__ __launch_bounds__(S::threads) void k_product(Product a, Finish finish)
+{
+    product<ELEM, PLANES, false, false, S>(a, finish, (int)blockIdx.x, (int)gridDim.x);
 }
 
 // --- what becomes of the results -------------------------------------------
@@ -782,6 +788,45 @@ struct FinishPart {
         }
     }
 };
+
+// A gradient whole or in parts.
+template <class OUT> struct FinishOut {
+    FinishStore<OUT> store;
+    FinishPart part;
+    bool in_parts;
+    template <class S> struct Rows {};
+    template <class S> __device__ __forceinline__ void fetch(const Product &, const Place &, Rows<S> &) const {}
+    template <class ELEM, class S>
+    __device__ __forceinline__ void operator()(const Product &a, const Place &at, const Rows<S> &,
+                                               f32x4 (&acc)[S::SP][S::SQ]) const
+    {
+        if (in_parts)
+            part.template operator()<ELEM, S>(a, at, FinishPart::Rows<S>{}, acc);
+        else
+            store.template operator()<ELEM, S>(a, at, typename FinishStore<OUT>::template Rows<S>{}, acc);
+    }
+};
+
+template <class OUT> struct GradJob {
+    Product a;
+    FinishOut<OUT> out;
+    int blocks; // 0: not wanted
+};
+
+// Both gradients of a piece, x's [rows][dim] = G [rows][classes] w [classes][dim]
+// and w's [classes][dim] = G^T [classes][rows] x [rows][dim], in one launch: each
+// alone often leaves compute units without a tile, or in a last round with few.
+template <class ELEM, bool PLANES, class S, class OUT>
+__global__ __launch_bounds__(S::threads) void k_gradients(GradJob<OUT> x, GradJob<OUT> w, bool w_first)
+{
+    const int first = w_first ? w.blocks : x.blocks;
+    const bool second = (int)blockIdx.x >= first;
+    const int block = (int)blockIdx.x - (second ? first : 0);
+    if (second != w_first)
+        product<ELEM, PLANES, true, true, S>(w.a, w.out, block, w.blocks);
+    else
+        product<ELEM, PLANES, true, false, S>(x.a, x.out, block, x.blocks);
+}
 
 // ---------------------------------------------------------------------------
 // the kernels around the products
@@ -1215,31 +1260,63 @@ Kind choose(int64_t p, int64_t q, int64_t batches, bool forward)
         return Kind::narrow;
     return large_tiles(p, q, batches) ? Kind::large : Kind::medium;
 }
-// The same for the gradients, whose p axis is the features and whose sums, over
-// `steps` steps, may be cut into parts: no more than 64 features would leave half
-// of a 128 wide tile empty; else the tile and the parts that end first, in steps
-// of the large tile: rounds, and each part's results written and read again in
-// float32 (at about 4 TB/s, 6 MB a step).
+// The tile and the parts of the gradients' launch, whose p axis is the features:
+// x's sums run over steps_x steps of classes, w's over steps_w of rows, and may be
+// cut into parts. No more than 64 features would leave half of a 128 wide tile
+// empty; else the tile and the parts that end first, in steps of the large tile:
+// the workgroups' steps as they follow each other on the compute units, and each
+// part's results written and read again in float32 (at about 4 TB/s, 6 MB a step).
 struct Cut {
     Kind kind;
-    int splits;
+    int split_x, split_w;
+    bool w_first; // the side with the longer workgroups
 };
-Cut choose_grad(int64_t dim, int64_t q, int64_t batches, int64_t steps, int planes)
+// When n1 jobs of d1 steps and then n2 of d2 end on so many slots.
+double end_of(int64_t n1, double d1, int64_t n2, double d2, int64_t slots)
 {
+    const int64_t rounds = n1 / slots, last = n1 % slots;
+    const double t = (double)rounds * d1, one = t + (last ? d1 : 0.0);
+    if (n2 == 0)
+        return one;
+    const double k = (double)ceil_to(n2, slots - last); // rounds of the slots that are free first
+    if (k * d2 <= d1 || last == 0)
+        return std::max(one, t + k * d2);
+    return t + std::ceil(((double)n2 + (double)last * (d1 / d2)) / (double)slots) * d2;
+}
+Cut choose_grads(int64_t dim, int64_t rows, int64_t classes, int64_t batches, int64_t steps_x, int64_t steps_w,
+                 int planes, bool want_x, bool want_w)
+{
+    static constexpr int cuts[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64};
     const int64_t least = planes > 1 ? 2 : 8; // a float32 step is six
-    const double work = (double)steps * (planes > 1 ? kPlaneProducts : 1);
-    Cut best{Kind::medium, 1};
+    const double each = planes > 1 ? kPlaneProducts : 1;
+    Cut best{Kind::medium, 1, 1, false};
     double least_cost = HUGE_VAL;
     // slots: workgroups that run at once; round: their step's time
     const auto consider = [&](Kind kind, int tile_p, int tile_q, int64_t slots, double round) {
-        const int64_t tiles = ceil_to(dim, tile_p) * (int64_t)ceil_to(q, tile_q) * batches;
-        const int64_t most = std::max<int64_t>(1, std::min<int64_t>({2 * slots / tiles, steps / least, 64}));
-        for (int64_t cut = 1; cut <= most; ++cut) {
-            const double join = cut > 1 ? (double)(cut + 1) * dim * q * batches * 8.0 / 6e6 + 4.0 : 0.0;
-            const double c = (double)ceil_to(tiles * cut, slots) * ((work + cut - 1) / cut + 4.0) * round + join;
-            if (c < least_cost) {
-                least_cost = c;
-                best = {kind, (int)cut};
+        const int64_t x = want_x ? ceil_to(dim, tile_p) * (int64_t)ceil_to(rows, tile_q) * batches : 0;
+        const int64_t w = want_w ? ceil_to(dim, tile_p) * (int64_t)ceil_to(classes, tile_q) * batches : 0;
+        const auto most = [&](int64_t tiles, int64_t steps) {
+            return tiles ? std::max<int64_t>(1, std::min<int64_t>({2 * slots / tiles, steps / least, 64})) : 1;
+        };
+        const auto join = [&](int cut, int64_t q) {
+            return cut > 1 ? (double)(cut + 1) * (double)(dim * q * batches) * 8.0 / 6e6 + 4.0 : 0.0;
+        };
+        const int64_t most_x = most(x, steps_x), most_w = most(w, steps_w);
+        for (const int cx : cuts) {
+            if (cx > most_x)
+                break;
+            const double dx = ((double)ceil_to(steps_x, cx) * each + 4.0) * round, jx = join(cx, rows);
+            for (const int cw : cuts) {
+                if (cw > most_w)
+                    break;
+                const double dw = ((double)ceil_to(steps_w, cw) * each + 4.0) * round;
+                const bool w_first = dw > dx;
+                const double c = (w_first ? end_of(w * cw, dw, x * cx, dx, slots) : end_of(x * cx, dx, w * cw, dw, slots)) +
+                                 jx + join(cw, classes);
+                if (c < least_cost) {
+                    least_cost = c;
+                    best = {kind, cx, cw, w_first};
+                }
             }
         }
     };
@@ -1254,30 +1331,50 @@ Cut choose_grad(int64_t dim, int64_t q, int64_t batches, int64_t steps, int plan
 int tile_p(Kind k) { return k == Kind::large ? 256 : k == Kind::thin ? 64 : 128; }
 int waves_p(Kind k) { return k == Kind::narrow ? Narrow::WP : 2; }
 
-template <class ELEM, bool PLANES, bool PK, bool QK, class S, class F>
-void launch_shape(Product a, int64_t cover_p, int64_t cover_q, const F &f, hipStream_t s)
+template <class S> int cover(Product &a, int64_t p, int64_t q)
 {
-    a.tiles_p = ceil_to(cover_p, S::TP);
-    a.tiles_q = ceil_to(cover_q, S::TQ);
+    a.tiles_p = ceil_to(p, S::TP);
+    a.tiles_q = ceil_to(q, S::TQ);
     a.group = std::min(a.tiles_q, 8);
-    const void *k = (const void *)k_product<ELEM, PLANES, PK, QK, S, F>;
-    (void)set_dynamic_lds(k, S::lds);
-    const int64_t grid = (int64_t)a.tiles_p * a.tiles_q * a.samples * a.splits;
-    k_product<ELEM, PLANES, PK, QK, S, F><<<dim3((unsigned)grid), dim3(S::threads), S::lds, s>>>(a, f);
+    return (int)((int64_t)a.tiles_p * a.tiles_q * a.samples * a.splits);
 }
 
-template <class ELEM, bool PLANES, bool PK, bool QK, class F>
+template <class ELEM, bool PLANES, class S, class F>
+void launch_shape(Product a, int64_t cover_p, int64_t cover_q, const F &f, hipStream_t s)
+{
+    const int grid = cover<S>(a, cover_p, cover_q);
+    (void)set_dynamic_lds((const void *)k_product<ELEM, PLANES, S, F>, S::lds);
+    k_product<ELEM, PLANES, S, F><<<dim3(grid), dim3(S::threads), S::lds, s>>>(a, f);
+}
+
+template <class ELEM, bool PLANES, class F>
 void launch_product(Kind kind, const Product &a, int64_t cover_p, int64_t cover_q, const F &f, hipStream_t s)
 {
     if (kind == Kind::large)
-        launch_shape<ELEM, PLANES, PK, QK, std::conditional_t<PK, Tall, Large>>(a, cover_p, cover_q, f, s);
+        launch_shape<ELEM, PLANES, Large>(a, cover_p, cover_q, f, s);
     else if (kind == Kind::medium)
-        launch_shape<ELEM, PLANES, PK, QK, Medium>(a, cover_p, cover_q, f, s);
-    else if (kind == Kind::thin) {
-        if constexpr (PK)
-            launch_shape<ELEM, PLANES, PK, QK, std::conditional_t<PLANES, ThinTriple, Thin>>(a, cover_p, cover_q, f, s);
-    } else if constexpr (std::is_same_v<F, FinishStats>)
-        launch_shape<ELEM, PLANES, PK, QK, Narrow>(a, cover_p, cover_q, f, s);
+        launch_shape<ELEM, PLANES, Medium>(a, cover_p, cover_q, f, s);
+    else if constexpr (std::is_same_v<F, FinishStats>)
+        launch_shape<ELEM, PLANES, Narrow>(a, cover_p, cover_q, f, s);
+}
+
+template <class ELEM, bool PLANES, class OUT>
+void launch_gradients(const Cut &cut, GradJob<OUT> x, GradJob<OUT> w, bool want_x, bool want_w, hipStream_t s)
+{
+    const auto with = [&](auto shape) {
+        using S = decltype(shape);
+        x.blocks = want_x ? cover<S>(x.a, x.a.p.rows, x.a.q.rows) : 0;
+        w.blocks = want_w ? cover<S>(w.a, w.a.p.rows, w.a.q.rows) : 0;
+        const auto k = k_gradients<ELEM, PLANES, S, OUT>;
+        (void)set_dynamic_lds((const void *)k, S::lds);
+        k<<<dim3(x.blocks + w.blocks), dim3(S::threads), S::lds, s>>>(x, w, cut.w_first);
+    };
+    if (cut.kind == Kind::large)
+        with(Tall{});
+    else if (cut.kind == Kind::medium)
+        with(Medium{});
+    else
+        with(std::conditional_t<PLANES, ThinTriple, Thin>{});
 }
 
 struct Offsets {
@@ -1454,9 +1551,9 @@ void ce_forward(const CeProblem &p, const CeForwardPlan &plan, uint8_t *ws, floa
         a.samples = p.samples;
         a.splits = 1;
         if (p.rows <= 16)
-            launch_shape<F32, false, false, false, Narrow>(a, p.classes, p.rows, finish, s);
+            launch_shape<F32, false, Narrow>(a, p.classes, p.rows, finish, s);
         else
-            launch_shape<F32, false, false, false, Medium>(a, p.classes, p.rows, finish, s);
+            launch_shape<F32, false, Medium>(a, p.classes, p.rows, finish, s);
     } else by_type(p.type, [&](auto elem, auto cut, auto io) {
         using ELEM = decltype(elem);
         using IO = decltype(io);
@@ -1474,8 +1571,8 @@ void ce_forward(const CeProblem &p, const CeForwardPlan &plan, uint8_t *ws, floa
         a.steps = plan.dim_pad / kCeStep;
         a.samples = p.samples;
         a.splits = 1;
-        launch_product<ELEM, decltype(cut)::value, false, false>(choose(p.classes, p.rows, p.samples, true), a,
-                                                                 p.classes, p.rows, finish, s);
+        launch_product<ELEM, decltype(cut)::value>(choose(p.classes, p.rows, p.samples, true), a, p.classes, p.rows,
+                                                   finish, s);
     });
     const auto join = [&](auto threads) {
         constexpr int T = decltype(threads)::value;
@@ -1499,14 +1596,11 @@ namespace {
 // float32 1.37, 1.20, 1.12, 1.33 ms).
 constexpr int64_t kPieceBytes = (int64_t)256 << 20;
 
-// The products for grad_x and grad_w of a whole piece.
-Cut cut_x(const CeProblem &p, const CeBackwardPlan &b)
+// The gradients' launch of a whole piece.
+Cut cut_of(const CeProblem &p, const CeBackwardPlan &b, bool want_x, bool want_w)
 {
-    return choose_grad(p.dim, p.rows, b.piece_samples, b.ld_g / kCeStep, planes(p));
-}
-Cut cut_w(const CeProblem &p, const CeBackwardPlan &b)
-{
-    return choose_grad(p.dim, b.piece_classes, b.piece_samples, b.rows_pad / kCeStep, planes(p));
+    return choose_grads(p.dim, p.rows, b.piece_classes, b.piece_samples, ceil_to(b.piece_classes, kCeStep),
+                        b.rows_pad / kCeStep, planes(p), want_x, want_w);
 }
 
 } // namespace
@@ -1533,8 +1627,9 @@ CeBackwardPlan ce_plan_backward(const CeProblem &p, bool want_x, bool want_w)
     // 16384 x 256: 3.42 ms, so 3.32; float32's three planes 0.89 and 0.90 ms)
     if (p.type != ElemType::f32 && b.ld_g % 1024 == 0)
         b.ld_g += 192;
-    b.split_x = cut_x(p, b).splits;
-    b.split_w = cut_w(p, b).splits;
+    const Cut cut = cut_of(p, b, want_x, want_w);
+    b.split_x = cut.split_x;
+    b.split_w = cut.split_w;
     b.sum_x = b.split_x > 1 || b.piece_classes < p.classes;
     const int64_t ld = pad_to(p.dim, 4);
     Offsets o;
@@ -1549,6 +1644,9 @@ CeBackwardPlan ce_plan_backward(const CeProblem &p, bool want_x, bool want_w)
     b.part_x = o.take(want_x && b.sum_x ? (int64_t)b.split_x * b.piece_samples * p.rows * ld * 4 : 0);
     b.part_w = o.take(want_w && b.split_w > 1 ? (int64_t)b.split_w * b.piece_samples * b.piece_classes * ld * 4 : 0);
     b.bytes = o.at;
+    // alone a gradient may be cut into more parts: room for both is room for either
+    if (want_x && want_w)
+        b.bytes = std::max({b.bytes, ce_plan_backward(p, true, false).bytes, ce_plan_backward(p, false, true).bytes});
     return b;
 }
 
@@ -1589,6 +1687,7 @@ void ce_backward(const CeProblem &p, const CeBackwardPlan &plan, uint8_t *ws, co
         packs.launch<IO>(s);
         const Operand W = features(p, plan.pack_w, p.w, w, p.classes, plan.dim_pad);
         const Operand X = features(p, plan.pack_x, p.x, x, p.rows, plan.dim_pad);
+        const Cut cut_grads = cut_of(p, plan, grad_x, grad_w);
         Joins joins;
         joins.jobs.cols = p.dim;
         joins.jobs.ld = (int)ld;
@@ -1611,7 +1710,7 @@ void ce_backward(const CeProblem &p, const CeBackwardPlan &plan, uint8_t *ws, co
                     a.samples = ns;
                     a.splits = 1;
                     const int64_t r0 = (int64_t)s0 * p.rows;
-                    launch_product<ELEM, PLANES, false, false>(
+                    launch_product<ELEM, PLANES>(
                         choose(nc, p.rows, ns, false), a, nc_pad, plan.rows_pad,
                         FinishGrad<PLANES>{target, coef, r0, g, plane_g, scale2_of(p), plan.rows_pad, plan.ld_g, c0}, s);
                 }
@@ -1620,8 +1719,9 @@ void ce_backward(const CeProblem &p, const CeBackwardPlan &plan, uint8_t *ws, co
                 G.sample = (int64_t)plan.rows_pad * plan.ld_g;
                 G.plane = plane_g;
                 G.ld = plan.ld_g;
-                if (grad_x) { // [rows][dim] = G [rows][classes] w [classes][dim]
-                    Product a{};
+                GradJob<IO> jx{}, jw{};
+                {
+                    Product &a = jx.a;
                     a.p = W;
                     a.p.base += s0 * W.sample + (int64_t)c0 * W.ld;
                     a.p.rows = p.dim;
@@ -1631,24 +1731,17 @@ void ce_backward(const CeProblem &p, const CeBackwardPlan &plan, uint8_t *ws, co
                     a.q.k = nc_pad;
                     a.steps = nc_pad / kCeStep;
                     a.samples = ns;
-                    const Kind kind = cut_x(p, plan).kind;
-                    if (plan.sum_x) {
-                        a.splits = plan.split_x;
-                        const int64_t sample = (int64_t)p.rows * ld, split = plan.piece_samples * sample;
-                        launch_product<ELEM, PLANES, true, false>(kind, a, p.dim, p.rows,
-                                                                  FinishPart{part_x, split, sample, (int)ld, c0 > 0}, s);
-                    } else {
-                        a.splits = 1;
-                        const int64_t sample = (int64_t)p.rows * p.dim;
-                        launch_product<ELEM, PLANES, true, false>(
-                            kind, a, p.dim, p.rows,
-                            FinishStore<IO>{(uint8_t *)grad_x + s0 * sample * elem_size(p.type),
-                                            coef + (int64_t)s0 * p.rows, top, inv_unit, sample},
-                            s);
-                    }
+                    a.splits = plan.split_x;
+                    const int64_t part = (int64_t)p.rows * ld, whole = (int64_t)p.rows * p.dim;
+                    jx.out.in_parts = plan.sum_x;
+                    jx.out.part = FinishPart{part_x, plan.piece_samples * part, part, (int)ld, c0 > 0};
+                    jx.out.store = FinishStore<IO>{(uint8_t *)grad_x + s0 * whole * elem_size(p.type),
+                                                   coef + (int64_t)s0 * p.rows, top, inv_unit, whole};
                 }
-                if (grad_w) { // [classes][dim] = G^T [classes][rows] x [rows][dim]
-                    Product a{};
+                const int64_t part = (int64_t)nc * ld, whole = (int64_t)p.classes * p.dim;
+                void *to = (uint8_t *)grad_w + (s0 * whole + (int64_t)c0 * p.dim) * elem_size(p.type);
+                {
+                    Product &a = jw.a;
                     a.p.base = xs + (int64_t)s0 * plan.rows_pad * plan.dim_pad;
                     a.p.sample = (int64_t)plan.rows_pad * plan.dim_pad;
                     a.p.plane = p.samples * a.p.sample;
@@ -1661,21 +1754,16 @@ void ce_backward(const CeProblem &p, const CeBackwardPlan &plan, uint8_t *ws, co
                     a.steps = plan.rows_pad / kCeStep;
                     a.samples = ns;
                     a.splits = plan.split_w;
-                    const Kind kind = cut_w(p, plan).kind;
-                    const int64_t sample = (int64_t)p.classes * p.dim;
-                    void *to = (uint8_t *)grad_w + (s0 * sample + (int64_t)c0 * p.dim) * elem_size(p.type);
-                    if (plan.split_w > 1) {
-                        const int64_t per = (int64_t)nc * ld, split = ns * per;
-                        launch_product<ELEM, PLANES, true, true>(kind, a, p.dim, nc,
-                                                                 FinishPart{part_w, split, per, (int)ld, false}, s);
-                        // several samples only where a piece holds all their classes
-                        joins.add(part_w, to, (int64_t)ns * nc, split, plan.split_w, nullptr);
-                        if (c0 + plan.piece_classes < p.classes)
-                            joins.launch<IO>(s); // before its parts are written over
-                    } else {
-                        launch_product<ELEM, PLANES, true, true>(kind, a, p.dim, nc,
-                                                                 FinishStore<IO>{to, nullptr, top, inv_unit, sample}, s);
-                    }
+                    jw.out.in_parts = plan.split_w > 1;
+                    jw.out.part = FinishPart{part_w, ns * part, part, (int)ld, false};
+                    jw.out.store = FinishStore<IO>{to, nullptr, top, inv_unit, whole};
+                }
+                launch_gradients<ELEM, PLANES>(cut_grads, jx, jw, grad_x, grad_w, s);
+                if (grad_w && plan.split_w > 1) {
+                    // several samples only where a piece holds all their classes
+                    joins.add(part_w, to, (int64_t)ns * nc, ns * part, plan.split_w, nullptr);
+                    if (c0 + plan.piece_classes < p.classes)
+                        joins.launch<IO>(s); // before its parts are written over
                 }
             }
             if (grad_x && plan.sum_x) {
