@@ -1614,7 +1614,8 @@ CeBackwardPlan ce_plan_backward(const CeProblem &p, bool want_x, bool want_w)
     const int64_t n = all_rows(p), size = 2 * planes(p);
     const int64_t whole = (int64_t)b.rows_pad * pad_to(p.classes, kCeStep) * size; // of one sample
     if (whole <= kPieceBytes) {
-        b.piece_samples = (int)std::min<int64_t>(p.samples, kPieceBytes / whole);
+        const int pieces = ceil_to(p.samples, kPieceBytes / whole); // of about as many samples each
+        b.piece_samples = ceil_to(p.samples, pieces);
         b.piece_classes = p.classes;
     } else {
         b.piece_samples = 1;
