@@ -58,6 +58,7 @@ struct CeBackwardPlan {
     int piece_samples, piece_classes; // the part of the logits' gradient that exists at a time
     int ld_g;                    // elements of a row of it, a multiple of kCeStep
     int split_x, split_w;        // parts of the sum over the classes (grad_x) and over the rows (grad_w)
+    bool whole_g;                // it holds float32 values as they are, else planes or 16-bit values
     bool sum_x;                  // grad_x is summed in float32 over several pieces or parts
     int tops;                    // workgroups of the pass over the upstream gradients (0: all rows have the same)
     size_t x, w, coef, block_top, top, xs, g, part_x, part_w, bytes;

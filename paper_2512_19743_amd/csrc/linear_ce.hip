@@ -8,7 +8,7 @@
 //
 // Four products of rows x classes x dim: z in the forward pass, z again in the
 // backward pass (by pieces, turned into dz in registers), dz w and dz^T x. All
-// run on one matrix-core kernel over 16-bit operands (k_product); what differs
+// run on the same matrix-core tiles of 16-bit operands (product()); what differs
 // is how each operand lies in memory and what becomes of the result.
 //
 // float32 operands are cut into three bfloat16 planes of 8 significant bits
@@ -175,6 +175,23 @@ __device__ __forceinline__ uint32_t tile_offset(const Operand &o, int r0, int j,
     }
 }
 
+// The same for an operand of float32 values (ld and base in 16-bit elements), of
+// 16 chunks a row with k contiguous, else ROWS / 4 chunks: chunk c of row r in slot
+// c ^ (r & 15), or of k in c ^ 4 (k / 8 & 3).
+template <bool KS> __device__ __forceinline__ int float_swizzle(int r) { return KS ? (r >> 1) & 12 : r & 15; }
+template <int ROWS, bool KS> __device__ __forceinline__ uint32_t float_offset(const Operand &o, int r0, int j, int lane, int k_left)
+{
+    constexpr int CH = KS ? ROWS / 4 : 16;
+    const int r = j * (64 / CH) + lane / CH, c = (lane % CH) ^ float_swizzle<KS>(r);
+    if constexpr (!KS) {
+        const int row = min(r0 + r, o.rows - 1);
+        return (uint32_t)((row - first_row<KS>(o, r0)) * o.ld) * 2u + min(c, (k_left - 1) >> 2) * 16u;
+    } else {
+        const int col = min(r0 + c * 4, (o.rows - 1) & ~3);
+        return (uint32_t)(min(r, k_left - 1) * o.ld) * 2u + (col - first_row<KS>(o, r0)) * 4u;
+    }
+}
+
 template <class T> using lds_ptr = __attribute__((address_space(3))) T *;
 
 // Orders a wave's own accesses to shared memory.
@@ -238,21 +255,53 @@ __device__ __forceinline__ i16x8 fragment(const lds_char *tile, int r0, int i, i
     }
 }
 
+// The three planes of such a fragment of float32 values.
+template <int ROWS, bool KS>
+__device__ __forceinline__ void float_fragment(const lds_char *tile, int r0, int i, int h, int lane, i16x8 (&planes)[3])
+{
+    const int r = r0 + i * 16 + (lane & 15), k = h * 32 + (lane >> 4) * 8;
+    float v[8];
+    if constexpr (!KS) {
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+            const f32x4 x = *(const __attribute__((address_space(3))) f32x4 *)(tile + r * 256 +
+                                                                                (((k >> 2) + c) ^ float_swizzle<KS>(r)) * 16);
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+                v[c * 4 + u] = x[u];
+        }
+    } else {
+        const lds_char *at = tile + k * (ROWS * 4) + (((r >> 2) ^ float_swizzle<KS>(k)) << 4) + ((r & 3) << 2);
+#pragma unroll
+        for (int u = 0; u < 8; ++u)
+            v[u] = *(const __attribute__((address_space(3))) float *)(at + u * (ROWS * 4));
+    }
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+        const Planes x = planes_of(v[u]);
+        planes[0][u] = (short)x.a;
+        planes[1][u] = (short)x.b;
+        planes[2][u] = (short)x.c;
+    }
+}
+
 // The tile shapes. A workgroup takes TP x TQ results, its waves WP x WQ of them,
 // with BUFS steps' tiles in shared memory. WOVEN: the fragments of the next half
-// step are read between the matrix instructions of this one. TRIPLE, for float32:
-// a step's tile holds all three planes of both operands and gives all six
-// products, half of the loads that six steps of one plane each need.
+// step are read between the matrix instructions of this one. TRIPLE, for float32: a
+// step's tile holds all three planes of P and Q as it is, which is cut into planes
+// on its way to the matrix cores, and gives all six products.
 template <int TP_, int TQ_, int WP_, int WQ_, int BUFS_, bool WOVEN_ = false, bool TRIPLE_ = false> struct Shape {
     static constexpr int TP = TP_, TQ = TQ_, WP = WP_, WQ = WQ_, BUFS = BUFS_;
     static constexpr bool WOVEN = WOVEN_, TRIPLE = TRIPLE_;
     static_assert(!WOVEN || BUFS == 2, "two tiles in turn");
     static constexpr int waves = WP * WQ, threads = 64 * waves;
     static constexpr int SP = TP / WP / 16, SQ = TQ / WQ / 16; // 16 x 16 results of a wave
-    static constexpr int stage = (TP + TQ) * 128 * (TRIPLE ? 3 : 1);
+    static constexpr int at_q = TP * 128 * (TRIPLE ? 3 : 1); // bytes of P, then of Q
+    static constexpr int stage = at_q + TQ * 128 * (TRIPLE ? 2 : 1);
     static constexpr int lds = stage * BUFS;
     static constexpr int LP = TP / 8 / waves;                                    // loads of a wave for P
-    static constexpr int LQ = (TQ / 8 + waves - 1) / waves;                      // and for Q
+    static constexpr int KQ = TQ / 8 * (TRIPLE ? 2 : 1);                         // KB of Q
+    static constexpr int LQ = (KQ + waves - 1) / waves;                          // and for Q
 };
 
 struct Place {
@@ -312,11 +361,15 @@ __device__ __forceinline__ void product(const Product &a, const Finish &finish, 
             op[j] = tile_offset<S::TP, PK, !PK>(a.p, at.p0, wave * S::LP + j, lane, kp);
 #pragma unroll
         for (int j = 0; j < S::LQ; ++j)
-            oq[j] = tile_offset<S::TQ, QK, false>(a.q, at.q0, (wave * S::LQ + j) % (S::TQ / 8), lane, kq);
+            if constexpr (S::TRIPLE)
+                oq[j] = float_offset<S::TQ, QK>(a.q, at.q0, (wave * S::LQ + j) % S::KQ, lane, kq);
+            else
+                oq[j] = tile_offset<S::TQ, QK, false>(a.q, at.q0, (wave * S::LQ + j) % S::KQ, lane, kq);
     };
-    const int64_t step_p = PK ? kCeStep * a.p.ld : kCeStep, step_q = QK ? kCeStep * a.q.ld : kCeStep;
+    constexpr int size_q = S::TRIPLE ? 2 : 1; // in 16-bit elements
+    const int64_t step_p = PK ? kCeStep * a.p.ld : kCeStep, step_q = QK ? kCeStep * a.q.ld : kCeStep * size_q;
     const uint64_t base_p = (uint64_t)(a.p.base + at.sample * a.p.sample + first_row<PK>(a.p, at.p0) * (PK ? 1 : a.p.ld));
-    const uint64_t base_q = (uint64_t)(a.q.base + at.sample * a.q.sample + first_row<QK>(a.q, at.q0) * (QK ? 1 : a.q.ld));
+    const uint64_t base_q = (uint64_t)(a.q.base + at.sample * a.q.sample + first_row<QK>(a.q, at.q0) * (QK ? size_q : a.q.ld));
     // A step that ends beyond an operand's summed axis clamps its offsets.
     const int ragged = (a.p.k < a.steps * kCeStep || a.q.k < a.steps * kCeStep) ? a.steps - 1 : -1;
     offsets(0);
@@ -330,19 +383,18 @@ __device__ __forceinline__ void product(const Product &a, const Finish &finish, 
         }
         if (ragged >= 0 && (step == ragged || step == first))
             offsets(step);
-        uint32_t to = lds0 + (i % S::BUFS) * S::stage;
+        const uint32_t to = lds0 + (i % S::BUFS) * S::stage;
 #pragma unroll
         for (int plane = 0; plane < (S::TRIPLE ? 3 : 1); ++plane) {
             const i32x4 rp = buffer_at(base_p + 2 * (uint64_t)(step * step_p + (pp + plane) * a.p.plane));
-            const i32x4 rq = buffer_at(base_q + 2 * (uint64_t)(step * step_q + (pq + plane) * a.q.plane));
 #pragma unroll
             for (int j = 0; j < S::LP; ++j)
-                load_to_lds(rp, op[j], to + (wave * S::LP + j) * 1024);
-#pragma unroll
-            for (int j = 0; j < S::LQ; ++j)
-                load_to_lds(rq, oq[j], to + S::TP * 128 + ((wave * S::LQ + j) % (S::TQ / 8)) * 1024);
-            to += (S::TP + S::TQ) * 128;
+                load_to_lds(rp, op[j], to + plane * (S::TP * 128) + (wave * S::LP + j) * 1024);
         }
+        const i32x4 rq = buffer_at(base_q + 2 * (uint64_t)(step * step_q + pq * a.q.plane));
+#pragma unroll
+        for (int j = 0; j < S::LQ; ++j)
+            load_to_lds(rq, oq[j], to + S::at_q + ((wave * S::LQ + j) % S::KQ) * 1024);
     };
 
     // what the finish needs of its rows is on its way during the products
@@ -356,15 +408,17 @@ __device__ __forceinline__ void product(const Product &a, const Finish &finish, 
         for (int j = 0; j < S::SQ; ++j)
             acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 
-    const auto read = [&](int i, int h, i16x8 (&fp)[S::SP], i16x8 (&fq)[S::SQ], int plane = 0) {
-        const lds_char *tp = (const lds_char *)smem + (i % S::BUFS) * S::stage + plane * ((S::TP + S::TQ) * 128);
-        const lds_char *tq = tp + S::TP * 128;
-#pragma unroll
-        for (int j = 0; j < S::SQ; ++j)
-            fq[j] = fragment<S::TQ, QK, false>(tq, at.wq * (S::SQ * 16), j, h, lane);
+    const auto read_p = [&](const lds_char *tp, int h, i16x8 (&fp)[S::SP]) {
 #pragma unroll
         for (int k = 0; k < S::SP; ++k)
             fp[k] = fragment<S::TP, PK, !PK>(tp, at.wp * (S::SP * 16), k, h, lane);
+    };
+    const auto read = [&](int i, int h, i16x8 (&fp)[S::SP], i16x8 (&fq)[S::SQ]) {
+        const lds_char *tp = (const lds_char *)smem + (i % S::BUFS) * S::stage;
+#pragma unroll
+        for (int j = 0; j < S::SQ; ++j)
+            fq[j] = fragment<S::TQ, QK, false>(tp + S::at_q, at.wq * (S::SQ * 16), j, h, lane);
+        read_p(tp, h, fp);
     };
     const auto multiply = [&](const i16x8 (&fp)[S::SP], const i16x8 (&fq)[S::SQ]) {
 #pragma unroll
@@ -437,10 +491,19 @@ __device__ __forceinline__ void product(const Product &a, const Finish &finish, 
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 if constexpr (S::TRIPLE) {
+                    const lds_char *tile = (const lds_char *)smem + (i % S::BUFS) * S::stage;
                     i16x8 fp[3][S::SP], fq[3][S::SQ];
 #pragma unroll
+                    for (int j = 0; j < S::SQ; ++j) {
+                        i16x8 three[3];
+                        float_fragment<S::TQ, QK>(tile + S::at_q, at.wq * (S::SQ * 16), j, h, lane, three);
+#pragma unroll
+                        for (int plane = 0; plane < 3; ++plane)
+                            fq[plane][j] = three[plane];
+                    }
+#pragma unroll
                     for (int plane = 0; plane < 3; ++plane)
-                        read(i, h, fp[plane], fq[plane], plane);
+                        read_p(tile + plane * (S::TP * 128), h, fp[plane]);
                     multiply(fp[0], fq[0]);
                     multiply(fp[0], fq[1]);
                     multiply(fp[1], fq[0]);
@@ -580,13 +643,14 @@ struct CeTop {
 
 // Backward: the logits' gradient of a piece, rounded to the operands' type (the
 // products that follow take 16-bit operands; each value is off by half a step of
-// its own size at most, as the operands x and w themselves are), or in three
-// planes for float32.
-template <bool PLANES> struct FinishGrad {
+// its own size at most, as the operands x and w themselves are), or for float32 in
+// three planes or as it is.
+enum class Stored { narrow, planes, whole };
+template <Stored AS> struct FinishGrad {
     Targets target;
     const CeCoef *coef;
     int64_t row0;        // the piece's first row
-    uint16_t *g;         // [samples of the piece][rows_pad][ld]
+    uint16_t *g;         // [samples of the piece][rows_pad][ld] (whole: of float32)
     int64_t plane;
     float scale2;
     int rows_pad, ld, class0;
@@ -652,7 +716,8 @@ template <bool PLANES> struct FinishGrad {
                         acc[k][j][i] = v0 + class_of(k, i) >= a.p.rows ? 0.0f : acc[k][j][i];
             }
             const int q0 = at.q0 + at.wq * (S::SQ * 16) + j * 16;
-            uint16_t *to = g + ((int64_t)at.sample * rows_pad + q0) * ld + w0;
+            const int64_t first = ((int64_t)at.sample * rows_pad + q0) * ld + w0;
+            uint16_t *to = g + first;
             const auto write = [&](auto value, uint16_t *out) {
 #pragma unroll
                 for (int k = 0; k < S::SP; k += 2) {
@@ -672,7 +737,23 @@ template <bool PLANES> struct FinishGrad {
                 }
                 wave_lds();
             };
-            if constexpr (PLANES) {
+            if constexpr (AS == Stored::whole) {
+                constexpr int LF = W + 4;
+                static_assert(16 * LF * 4 <= S::lds / S::waves, "a wave's part of the tiles holds 16 rows");
+                const auto row = (lds_ptr<float>)at.lds;
+#pragma unroll
+                for (int k = 0; k < S::SP; ++k)
+                    *(lds_ptr<f32x4>)(row + (at.lane & 15) * LF + (k >> 1) * 32 + 8 * (at.lane >> 4) + (k & 1) * 4) = acc[k][j];
+                wave_lds();
+                const int n = min(16, rows_pad - q0) * (W / 4);
+#pragma unroll
+                for (int u = 0; u < W / 16; ++u) {
+                    const int i = at.lane + u * 64, r = i / (W / 4), c = i % (W / 4) * 4;
+                    if (i < n && w0 + c < ld)
+                        *(f32x4 *)((float *)g + first + (int64_t)r * ld + c) = *(lds_ptr<f32x4>)(row + r * LF + c);
+                }
+                wave_lds();
+            } else if constexpr (AS == Stored::planes) {
                 write([](float v) { return planes_of(v).a; }, to);
                 write([](float v) { return planes_of(v).b; }, to + plane);
                 write([](float v) { return planes_of(v).c; }, to + 2 * plane);
@@ -1232,7 +1313,7 @@ using Tall = Shape<256, 256, 4, 2, 2, true>;  // the gradients' (8192 x 4096 x 8
 using Medium = Shape<128, 128, 2, 2, 2>;
 using Narrow = Shape<128, 16, 4, 1, 4>;
 using Thin = Shape<64, 128, 2, 2, 2>;
-using ThinTriple = Shape<64, 128, 2, 4, 2, false, true>; // 10 of 64 x 2048 x 2048: 53 us; one plane a step 68
+using ThinTriple = Shape<64, 128, 2, 4, 2, false, true>; // 16 of 2048 x 2048 x 64: 156 us, with Q in planes 170
 
 int ceil_to(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
 int64_t pad_to(int64_t a, int64_t b) { return (a + b - 1) / b * b; }
@@ -1592,9 +1673,14 @@ namespace {
 // The piece of the logits' gradient that exists at a time: about what the 256 MB
 // last-level cache keeps between the product that writes it and the two that
 // read it. Smaller pieces are more launches, each with a tail (64, 128, 256, 512
-// MB: 16 x 4096 x 16384 x 256 4.21, 3.72, 3.45, 3.56 ms; 32 x 2048 x 2048 x 64
-// float32 1.37, 1.20, 1.12, 1.33 ms).
+// MB: 16 x 4096 x 16384 x 256 4.21, 3.72, 3.45, 3.56 ms before the gradients shared
+// a launch; 128 and 256 MB now: 32 x 2048 x 2048 x 64 float32 676 and 689 us, one
+// sample of 20000 x 20000 x 64 1895 and 1790).
 constexpr int64_t kPieceBytes = (int64_t)256 << 20;
+
+// Whether the logits' gradient is stored in float32 as it is, two thirds of its
+// planes: where the gradients' tile is ThinTriple.
+bool whole_gradient(const CeProblem &p) { return p.type == ElemType::f32 && p.dim <= 64; }
 
 // The gradients' launch of a whole piece.
 Cut cut_of(const CeProblem &p, const CeBackwardPlan &b, bool want_x, bool want_w)
@@ -1611,15 +1697,16 @@ CeBackwardPlan ce_plan_backward(const CeProblem &p, bool want_x, bool want_w)
     choose_packs(p, &b.pack_x, &b.pack_w);
     b.dim_pad = (int)pad_to(p.dim, kCeStep);
     b.rows_pad = (int)pad_to(p.rows, kCeStep);
-    const int64_t n = all_rows(p), size = 2 * planes(p);
-    const int64_t whole = (int64_t)b.rows_pad * pad_to(p.classes, kCeStep) * size; // of one sample
+    b.whole_g = whole_gradient(p);
+    const int64_t n = all_rows(p), size = 2 * planes(p), size_g = b.whole_g ? 4 : size;
+    const int64_t whole = (int64_t)b.rows_pad * pad_to(p.classes, kCeStep) * size_g; // of one sample
     if (whole <= kPieceBytes) {
         const int pieces = ceil_to(p.samples, kPieceBytes / whole); // of about as many samples each
         b.piece_samples = ceil_to(p.samples, pieces);
         b.piece_classes = p.classes;
     } else {
         b.piece_samples = 1;
-        const int64_t most = std::max<int64_t>(256, kPieceBytes / (b.rows_pad * size) / 256 * 256);
+        const int64_t most = std::max<int64_t>(256, kPieceBytes / (b.rows_pad * size_g) / 256 * 256);
         const int pieces = ceil_to(p.classes, most);
         b.piece_classes = (int)std::min<int64_t>(p.classes, pad_to(ceil_to(p.classes, pieces), 256));
     }
@@ -1641,7 +1728,7 @@ CeBackwardPlan ce_plan_backward(const CeProblem &p, bool want_x, bool want_w)
     b.block_top = o.take(b.tops * sizeof(float2));
     b.top = o.take(sizeof(CeTop));
     b.xs = o.take(want_w ? (int64_t)p.samples * b.rows_pad * b.dim_pad * size : 0);
-    b.g = o.take((int64_t)b.piece_samples * b.rows_pad * b.ld_g * size);
+    b.g = o.take((int64_t)b.piece_samples * b.rows_pad * b.ld_g * size_g);
     b.part_x = o.take(want_x && b.sum_x ? (int64_t)b.split_x * b.piece_samples * p.rows * ld * 4 : 0);
     b.part_w = o.take(want_w && b.split_w > 1 ? (int64_t)b.split_w * b.piece_samples * b.piece_classes * ld * 4 : 0);
     b.bytes = o.at;
@@ -1711,15 +1798,28 @@ void ce_backward(const CeProblem &p, const CeBackwardPlan &plan, uint8_t *ws, co
                     a.samples = ns;
                     a.splits = 1;
                     const int64_t r0 = (int64_t)s0 * p.rows;
-                    launch_product<ELEM, PLANES>(
-                        choose(nc, p.rows, ns, false), a, nc_pad, plan.rows_pad,
-                        FinishGrad<PLANES>{target, coef, r0, g, plane_g, scale2_of(p), plan.rows_pad, plan.ld_g, c0}, s);
+                    const auto product = [&](auto as) {
+                        launch_product<ELEM, PLANES>(choose(nc, p.rows, ns, false), a, nc_pad, plan.rows_pad,
+                                                     FinishGrad<decltype(as)::value>{target, coef, r0, g, plane_g,
+                                                                                     scale2_of(p), plan.rows_pad,
+                                                                                     plan.ld_g, c0}, s);
+                    };
+                    if constexpr (!PLANES)
+                        product(std::integral_constant<Stored, Stored::narrow>{});
+                    else if (plan.whole_g)
+                        product(std::integral_constant<Stored, Stored::whole>{});
+                    else
+                        product(std::integral_constant<Stored, Stored::planes>{});
                 }
                 Operand G;
                 G.base = g;
                 G.sample = (int64_t)plan.rows_pad * plan.ld_g;
                 G.plane = plane_g;
                 G.ld = plan.ld_g;
+                if (plan.whole_g) { // in 16-bit elements
+                    G.sample *= 2;
+                    G.ld *= 2;
+                }
                 GradJob<IO> jx{}, jw{};
                 {
                     Product &a = jx.a;
