@@ -525,3 +525,27 @@ def test_scored_without_gradients(mode):
     with mode():
         got = apml.linear_ce_loss(x, w.requires_grad_(), t, reduction="none")
     assert torch.equal(got, want) and not got.requires_grad
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("size", [(0, 64, 40000, 128), (0, 4100, 90, 200), (3, 333, 5001, 48), (0, 2000, 2000, 600)],
+                         ids=lambda s: "x".join(map(str, s)))
+def test_one_gradient_alone(size, dtype):
+    """Alone a gradient is cut into parts of its own."""
+    x, w, t = make(*size, dtype)
+    one = torch.ones((), device="cuda")
+    want = oracle.linear_ce(x, w, t)
+    _, state = apml.apml_linear_ce_forward(x, w, t)
+    gx, none = apml.apml_linear_ce_backward(state, x, w, t, one, want_grad_w=False)
+    oracle.within(gx, want["grad_x"], want["grad_x_tol"], "grad_x")
+    assert none is None
+    none, gw = apml.apml_linear_ce_backward(state, x, w, t, one, want_grad_x=False)
+    oracle.within(gw, want["grad_w"], want["grad_w_tol"], "grad_w")
+    assert none is None
+
+
+@pytest.mark.parametrize("size,dtype", [((5, 4096, 8192, 64), BF16), ((7, 2050, 8000, 33), F32), ((0, 5000, 30000, 64), F32)],
+                         ids=["3+2 of 5 samples", "4+3 of 7 samples", "pieces of the classes"])
+def test_pieces_of_unequal_size(size, dtype):
+    x, w, t = make(*size, dtype, ignored=0.1)
+    check(x, w, t, z_weight=1e-3)
