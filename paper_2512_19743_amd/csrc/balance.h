@@ -29,7 +29,7 @@ struct BalancePlan {
     size_t p, count, z, loss, ticket, bytes;
 };
 BalancePlan balance_plan(const BalanceProblem &p);
-// state: [samples][experts + 1] floats (E f_e, then 1 / valid tokens), or NULL.
+// state: [samples][experts + 1] floats (E (f_e - min f), then 1 / valid tokens), or NULL.
 // counts: written where index is given, else read.
 void balance_forward(const BalanceProblem &p, const BalancePlan &plan, uint8_t *ws, int64_t *counts, float *loss,
                      float *state, hipStream_t s);

@@ -330,3 +330,24 @@ def test_measured_without_gradients(mode):
     assert torch.equal(got, want) and torch.equal(again, want) and torch.equal(count, tokens)
     with pytest.raises(ValueError, match="number"):
         apml.balance_loss(logits, ids, valid=valid, z_weight=torch.zeros(()))
+
+
+@pytest.mark.parametrize("slots_dropped", [0.0, 1e-3, 0.05])
+@pytest.mark.parametrize("experts", [8, 21])
+def test_shares_that_are_nearly_equal(experts, slots_dropped):
+    """Every expert chosen by every token: the gradient is what is left of equal shares."""
+    logits, ids, valid = make(2, 3001, experts, experts, F32, dropped=slots_dropped, padded=0.2)
+    ids = torch.where(ids < 0, ids, torch.arange(experts, device="cuda"))
+    leaf = logits.clone().requires_grad_(True)
+    loss, counts = apml.balance_loss(leaf, ids, valid=valid)
+    got = torch.autograd.grad(loss, leaf)[0].double()
+    p = torch.where(valid.unsqueeze(-1), torch.softmax(logits.double(), -1), 0.0)
+    c = counts.double()
+    d = (experts * (c - c.amin(-1, keepdim=True)) / c.sum(-1, keepdim=True)).unsqueeze(1)
+    g = 1.0 / (2 * valid.sum(-1).double()).view(2, 1, 1)
+    dot = (p * d).sum(-1, keepdim=True)
+    # p is off by 3 * 2^-17 at most, the sum over the experts by a step each
+    tol = g * p * (d + dot) * (3 * 2.0 ** -17 + (experts + 16) * 2.0 ** -24) + 2.0 ** -149
+    assert ((got - g * p * (d - dot)).abs() <= tol).all()
+    if slots_dropped == 0.0:
+        assert (counts == counts[:, :1]).all() and not got.any()
