@@ -18,6 +18,7 @@
 
 #include "../../include/apml.h"
 #include "apml_internal.h"
+#include "errors.h"
 
 using namespace apml;
 

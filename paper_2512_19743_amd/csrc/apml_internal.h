@@ -7,8 +7,6 @@
 #include <cstddef>
 #include <cstdint>
 
-#include "../../include/apml.h"
-
 namespace apml {
 
 constexpr int kBlock = 256;       // threads per workgroup of the grid-wide kernels
@@ -359,10 +357,6 @@ hipError_t launch_csc_and_softmax(const DevPlan &d, const Params &p, int64_t max
 // device, made once per device and kernel for every larger size (the forward
 // and backward would otherwise make the runtime call on every call).
 hipError_t set_dynamic_lds(const void *k, size_t bytes);
-
-// The calling thread's error text (apml_last_error), for the entry points outside api.hip.
-apml_status fail_with(apml_status st, const char *msg);
-void clear_error();
 
 void launch_softmax(const DevPlan &d, const Params &p, hipStream_t s);
 // Backward of both softmaxes and the distance gradient. double_p: P formed

@@ -5,8 +5,8 @@
 #include <cstdio>
 
 #include "../../include/apml.h"
-#include "apml_internal.h"
 #include "balance.h"
+#include "errors.h"
 #include "linear_ce.h"
 
 using namespace apml;
