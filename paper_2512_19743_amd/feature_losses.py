@@ -91,7 +91,7 @@ def balance_loss(logits: torch.Tensor, experts: Optional[torch.Tensor] = None, *
     log-sum-exp; and the tokens per expert, int64.
 
     logits (B, tokens, experts), a loss per sample, or (tokens, experts), one sample; float32, bfloat16 or
-    float16 GPU tensors. experts (..., chosen): the experts that each token goes to, int64 or int32, -1 for
+    float16 GPU tensors, up to 1024 experts. experts (..., chosen): the experts that each token goes to, int64 or int32, -1 for
     a dropped slot. counts instead: the tokens per expert, (B, experts) or (experts,), for instance the sum
     of every rank's expert_counts. valid: bool, the tokens' shape, False for padding.
     The gradient flows into logits through the probabilities, not through the counts.
@@ -107,5 +107,6 @@ def balance_loss(logits: torch.Tensor, experts: Optional[torch.Tensor] = None, *
 
 def expert_counts(experts: torch.Tensor, num_experts: int, *, valid: Optional[torch.Tensor] = None) -> torch.Tensor:
     """Tokens per expert, int64 (B, num_experts) or (num_experts,), of experts (B, tokens, chosen) or
-    (tokens, chosen); entries outside [0, num_experts) are dropped slots, tokens that are not valid padding."""
+    (tokens, chosen); num_experts up to 1024. Entries outside [0, num_experts) are dropped slots, tokens that
+    are not valid padding."""
     return _lib.apml_expert_counts(experts.contiguous(), num_experts, valid=valid.contiguous() if valid is not None else None)
