@@ -779,10 +779,53 @@ template <class T, int N> struct __attribute__((packed, aligned(sizeof(T)))) Loo
     T v[N];
 };
 
+// What the rounding of the targets' entries took from x's gradient: a row's entry
+// for its target is as large as all the others together, so that its half step
+// was most of the gradient's error (4 x 4769 x 4507 x 64 bfloat16: 1.5 times that of
+// one rounding at the end, now 1.0). It goes back in as rest w_target; the gradient
+// of w, where a class adds up many rows' entries, goes without.
+template <class OUT> struct TargetRest {
+    Targets target;
+    const uint16_t *w;   // [samples][classes][dim] as the caller holds it
+    const CeCoef *coef;
+    int64_t row0;        // the rows of w's first sample begin here in target
+    int rows, dim;       // per sample
+    float inv_unit;
+    // v[u] += rest w_target[c + u] for u < n of row `row` from row0 on
+    template <int N> __device__ __forceinline__ void add(int64_t row, int c, int n, float (&v)[N]) const
+    {
+        const float entry = coef[row].at_target;
+        const float rest = (entry - OUT::to(OUT::from(entry))) * coef[row].unit * inv_unit;
+        const int t = target[row0 + row];
+        if (t < 0 || rest == 0.0f || !(fabsf(rest) < kInf)) // beyond float16's range the entry is infinite
+            return;
+        const uint16_t *from = w + (row / rows * target.classes + t) * dim + c;
+        if (n >= N) {
+            const Loose<uint16_t, N> x = *(const Loose<uint16_t, N> *)from;
+#pragma unroll
+            for (int u = 0; u < N; ++u)
+                v[u] = __builtin_fmaf(rest, OUT::to(x.v[u]), v[u]);
+        } else {
+            for (int u = 0; u < n; ++u)
+                v[u] = __builtin_fmaf(rest, OUT::to(from[u]), v[u]);
+        }
+    }
+};
+template <> struct TargetRest<float> { // all bits are kept
+    Targets target;
+    const uint16_t *w;
+    const CeCoef *coef;
+    int64_t row0;
+    int rows, dim;
+    float inv_unit;
+    template <int N> __device__ __forceinline__ void add(int64_t, int, int, float (&)[N]) const {}
+};
+
 // A gradient [samples][q rows][p rows]: rounded once and stored, times a factor
 // per row (coef) or for all (top).
 template <class OUT> struct FinishStore {
     void *out;
+    TargetRest<OUT> rest; // grad_x
     const CeCoef *coef; // grad_x: the rows' units, else NULL
     const CeTop *top;   // grad_w: the largest unit
     float inv_unit;     // 1 / ELEM::kUnit
@@ -820,15 +863,23 @@ template <class OUT> struct FinishStore {
                 const int r = i / (W / VEC), c = i % (W / VEC) * VEC, left = a.p.rows - p0 - c;
                 const lds_ptr<float> from = row + r * LD + c;
                 auto *at_out = (Element<OUT> *)out + to + (int64_t)r * a.p.rows + c;
-                if (left >= VEC) {
-                    Loose<Element<OUT>, VEC> v;
+                float x[VEC];
 #pragma unroll
-                    for (int u = 0; u < VEC; ++u)
-                        v.v[u] = element<OUT>(from[u]);
+                for (int u = 0; u < VEC; ++u)
+                    x[u] = from[u];
+                if (coef)
+                    rest.add((int64_t)at.sample * a.q.rows + q0 + j * 16 + r, p0 + c, left, x);
+                Loose<Element<OUT>, VEC> v;
+#pragma unroll
+                for (int u = 0; u < VEC; ++u)
+                    v.v[u] = element<OUT>(x[u]);
+                if (left >= VEC) {
                     *(Loose<Element<OUT>, VEC> *)at_out = v;
                 } else {
-                    for (int u = 0; u < left; ++u)
-                        at_out[u] = element<OUT>(from[u]);
+#pragma unroll
+                    for (int u = 0; u < VEC; ++u)
+                        if (u < left)
+                            at_out[u] = v.v[u];
                 }
             }
             wave_lds();
@@ -1279,13 +1330,14 @@ struct JoinJob {
     const CeCoef *coef;  // grad_x: the rows' units, else NULL
     unsigned blocks;
 };
-struct JoinJobs {
+template <class OUT> struct JoinJobs {
     JoinJob job[2];
+    TargetRest<OUT> rest;
     int cols, ld;
     const CeTop *top;
     float inv_unit;
 };
-template <class OUT> __global__ __launch_bounds__(kBlock) void k_ce_join(JoinJobs jobs)
+template <class OUT> __global__ __launch_bounds__(kBlock) void k_ce_join(JoinJobs<OUT> jobs)
 {
     const bool second = blockIdx.x >= jobs.job[0].blocks;
     const JoinJob &p = jobs.job[second];
@@ -1298,10 +1350,13 @@ template <class OUT> __global__ __launch_bounds__(kBlock) void k_ce_join(JoinJob
     for (int s = 1; s < p.splits; ++s)
         v += *(const f32x4 *)(p.part + s * p.split + i);
     v *= (p.coef ? p.coef[r].unit : jobs.top->top) * jobs.inv_unit;
+    float x[4] = {v[0], v[1], v[2], v[3]};
+    if (p.coef)
+        jobs.rest.add(r, c, jobs.cols - c, x);
 #pragma unroll
     for (int u = 0; u < 4; ++u)
         if (c + u < jobs.cols)
-            ((Element<OUT> *)p.out)[r * jobs.cols + c + u] = element<OUT>(v[u]);
+            ((Element<OUT> *)p.out)[r * jobs.cols + c + u] = element<OUT>(x[u]);
 }
 
 // ---------------------------------------------------------------------------
@@ -1522,14 +1577,14 @@ float scale2_of(const CeProblem &p)
 }
 
 // Gradients whose parts wait to be added up.
-struct Joins {
-    JoinJobs jobs{};
+template <class OUT> struct Joins {
+    JoinJobs<OUT> jobs{};
     int n = 0;
     void add(const float *part, void *out, int64_t rows, int64_t split, int splits, const CeCoef *coef)
     {
         jobs.job[n++] = JoinJob{part, out, rows, split, splits, coef, blocks_for(rows * jobs.ld / 4, kBlock)};
     }
-    template <class OUT> void launch(hipStream_t s)
+    void launch(hipStream_t s)
     {
         if (n)
             k_ce_join<OUT><<<dim3(jobs.job[0].blocks + (n > 1 ? jobs.job[1].blocks : 0)), dim3(kBlock), 0, s>>>(jobs);
@@ -1776,13 +1831,16 @@ void ce_backward(const CeProblem &p, const CeBackwardPlan &plan, uint8_t *ws, co
         const Operand W = features(p, plan.pack_w, p.w, w, p.classes, plan.dim_pad);
         const Operand X = features(p, plan.pack_x, p.x, x, p.rows, plan.dim_pad);
         const Cut cut_grads = cut_of(p, plan, grad_x, grad_w);
-        Joins joins;
+        Joins<IO> joins;
         joins.jobs.cols = p.dim;
         joins.jobs.ld = (int)ld;
         joins.jobs.top = top;
         joins.jobs.inv_unit = inv_unit;
         for (int s0 = 0; s0 < p.samples; s0 += plan.piece_samples) {
             const int ns = std::min(plan.piece_samples, p.samples - s0);
+            const TargetRest<IO> rest{target, (const uint16_t *)p.w + (int64_t)s0 * p.classes * p.dim,
+                                      coef + (int64_t)s0 * p.rows, (int64_t)s0 * p.rows, p.rows, p.dim, inv_unit};
+            joins.jobs.rest = rest;
             for (int c0 = 0; c0 < p.classes; c0 += plan.piece_classes) {
                 const int nc = std::min(plan.piece_classes, p.classes - c0);
                 const int nc_pad = (int)pad_to(nc, kCeStep);
@@ -1836,7 +1894,7 @@ void ce_backward(const CeProblem &p, const CeBackwardPlan &plan, uint8_t *ws, co
                     const int64_t part = (int64_t)p.rows * ld, whole = (int64_t)p.rows * p.dim;
                     jx.out.in_parts = plan.sum_x;
                     jx.out.part = FinishPart{part_x, plan.piece_samples * part, part, (int)ld, c0 > 0};
-                    jx.out.store = FinishStore<IO>{(uint8_t *)grad_x + s0 * whole * elem_size(p.type),
+                    jx.out.store = FinishStore<IO>{(uint8_t *)grad_x + s0 * whole * elem_size(p.type), rest,
                                                    coef + (int64_t)s0 * p.rows, top, inv_unit, whole};
                 }
                 const int64_t part = (int64_t)nc * ld, whole = (int64_t)p.classes * p.dim;
@@ -1857,14 +1915,14 @@ void ce_backward(const CeProblem &p, const CeBackwardPlan &plan, uint8_t *ws, co
                     a.splits = plan.split_w;
                     jw.out.in_parts = plan.split_w > 1;
                     jw.out.part = FinishPart{part_w, ns * part, part, (int)ld, false};
-                    jw.out.store = FinishStore<IO>{to, nullptr, top, inv_unit, whole};
+                    jw.out.store = FinishStore<IO>{to, rest, nullptr, top, inv_unit, whole};
                 }
                 launch_gradients<ELEM, PLANES>(cut_grads, jx, jw, grad_x, grad_w, s);
                 if (grad_w && plan.split_w > 1) {
                     // several samples only where a piece holds all their classes
                     joins.add(part_w, to, (int64_t)ns * nc, ns * part, plan.split_w, nullptr);
                     if (c0 + plan.piece_classes < p.classes)
-                        joins.launch<IO>(s); // before its parts are written over
+                        joins.launch(s); // before its parts are written over
                 }
             }
             if (grad_x && plan.sum_x) {
@@ -1872,7 +1930,7 @@ void ce_backward(const CeProblem &p, const CeBackwardPlan &plan, uint8_t *ws, co
                 joins.add(part_x, (uint8_t *)grad_x + (int64_t)s0 * p.rows * p.dim * elem_size(p.type),
                           (int64_t)ns * p.rows, split, plan.split_x, coef + (int64_t)s0 * p.rows);
             }
-            joins.launch<IO>(s); // while its parts are in the cache
+            joins.launch(s); // while its parts are in the cache
         }
     });
 }

@@ -549,3 +549,27 @@ def test_one_gradient_alone(size, dtype):
 def test_pieces_of_unequal_size(size, dtype):
     x, w, t = make(*size, dtype, ignored=0.1)
     check(x, w, t, z_weight=1e-3)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16], ids=["bf16", "f16"])
+@pytest.mark.parametrize("size", [(2, 300, 1500, 64), (0, 64, 40000, 128), (3, 129, 2000, 67), (0, 700, 1000, 200)],
+                         ids=lambda s: "x".join(map(str, s)))
+def test_the_targets_entries_lose_nothing_in_x(size, dtype):
+    """x's gradient is as near as one rounding of it: the roundings of the other classes' entries are
+    independent and each far below the row's, so that their squares add up to little."""
+    x, w, t = make(*size, dtype, ignored=0.1)
+    x, w = (torch.nn.functional.normalize(v.float(), dim=-1).to(dtype) for v in (x, w))
+    up = float(t.numel())  # float16: the gradient of a mean is below its normal range
+    leaf = x.clone().requires_grad_(True)
+    loss = apml.linear_ce_loss(leaf, w, t, scale=12.0)
+    got = torch.autograd.grad(loss, leaf, torch.tensor(up, device="cuda"))[0].double()
+    X, W, T = (v if w.dim() == 3 else v.unsqueeze(0) for v in (x.double(), w.double(), t))
+    used = T >= 0
+    at = T.clamp_min(0).unsqueeze(-1)
+    G = torch.softmax(12.0 * X @ W.transpose(1, 2).contiguous(), -1)
+    G = G.scatter(2, at, G.gather(2, at) - 1.0) * (12.0 * up / used.sum()) * used.unsqueeze(-1)
+    want = (G @ W).reshape(x.shape)
+    rounded = (want.to(dtype).double() - want).square().sum()
+    # an entry's rounding is off by u of it at most, u^2 / 3 in the mean of squares
+    others = (oracle.HALF[dtype] ** 2 / 3 * G.scatter(2, at, 0.0).square() * W.square().sum(-1).unsqueeze(1)).sum()
+    assert (got - want).square().sum() <= 1.2 * (rounded + others)
