@@ -376,7 +376,8 @@ apml_status apml_linear_ce_forward(const apml_linear_ce_desc *desc, const void *
  * (NONE) or one value; x, w, target and state as in the forward call. grad_x and
  * grad_w (shapes of x and w) are overwritten; one of them may be NULL. The logits'
  * gradient exists in pieces of the classes (or of the samples), rounded to x's
- * type for the two products that read it.
+ * type for the two products that read it; grad_x gets back what the rounding of
+ * its rows' targets took.
  */
 apml_status apml_linear_ce_backward(const apml_linear_ce_desc *desc, const void *x, const void *w, const void *target,
                                     const float *state, const float *grad_loss, void *grad_x, void *grad_w,
