@@ -1632,7 +1632,7 @@ bool ce_launches_fit(const CeProblem &p)
     choose_packs(p, &x, &w);
     const int64_t copied = (x ? all_rows(p) : 0) + (w ? (int64_t)p.samples * p.classes : 0) +
                            p.samples * pad_to(p.rows, kCeStep);
-    return rows * ceil_to(p.classes, 128) * 256 < limit && std::max(rows, classes) * features * 256 < limit &&
+    return rows * ceil_to(p.classes, 128) * 256 < limit && (rows + classes) * features * 256 < limit &&
            copied * dim_pad / 8 + all_rows(p) < limit && p.rows * pad_to(p.dim, 4) / 4 < limit;
 }
 
