@@ -631,7 +631,9 @@ struct FinishStats {
 
 // What the backward pass needs of a row: the logits' gradient is
 // fac exp2(z - top), or at_target for the target's class, in units of `unit`;
-// fac 0: an ignored row.
+// fac 0: an ignored row or one of no upstream gradient, with top 0, since its z are
+// taken as 0 (an ignored row's may be NaN) and exp2(0 - top) is infinite for a row
+// whose logits all lie below -128 log 2.
 struct CeCoef {
     float top, fac, at_target, unit;
 };
@@ -1070,6 +1072,8 @@ struct Coefs {
         CeCoef k{r.top, (bn + cn) * r.inv_total, cn * (1.0f - r.miss) - bn * r.miss, mine};
         if (at == kOutside)
             k.fac = __builtin_nanf("");
+        if (k.fac == 0.0f)
+            k.top = 0.0f;
         return k;
     }
 };

@@ -573,3 +573,23 @@ def test_the_targets_entries_lose_nothing_in_x(size, dtype):
     # an entry's rounding is off by u of it at most, u^2 / 3 in the mean of squares
     others = (oracle.HALF[dtype] ** 2 / 3 * G.scatter(2, at, 0.0).square() * W.square().sum(-1).unsqueeze(1)).sum()
     assert (got - want).square().sum() <= 1.2 * (rounded + others)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16, F16], ids=["f32", "bf16", "f16"])
+@pytest.mark.parametrize("low", [150.0, 1000.0])
+@pytest.mark.parametrize("size", [(0, 70, 200, 64), (0, 70, 200, 72), (2, 40, 90, 64), (0, 2048, 2100, 136)],
+                         ids=lambda s: "x".join(map(str, s)))
+def test_rows_of_no_weight_with_logits_far_below_zero(size, low, dtype):
+    """A row that counts and whose upstream gradient is 0 has a gradient of 0, wherever its logits lie."""
+    x, w, t = make(*size, dtype)
+    x[..., 0], w[..., 0] = 8.0, -low / 8.0
+    g = torch.rand(t.shape, device="cuda") + 0.5
+    g[..., ::3] = 0.0
+    for z_weight in (0.0, 0.01):
+        _, gx, _ = check(x, w, t, reduction="none", z_weight=z_weight, grad_loss=g)
+        assert (gx[..., ::3, :] == 0).all()
+        for reduction in ("none", "sum", "mean"):
+            off = torch.zeros(t.shape if reduction == "none" else (), device="cuda")
+            _, gx, gw = check(x, w, t, reduction=reduction, z_weight=z_weight, grad_loss=off)
+            assert (gx == 0).all() and (gw == 0).all()
+    check(x, w, t, z_weight=0.01)
