@@ -377,7 +377,9 @@ apml_status apml_linear_ce_forward(const apml_linear_ce_desc *desc, const void *
  * grad_w (shapes of x and w) are overwritten; one of them may be NULL. The logits'
  * gradient exists in pieces of the classes (or of the samples), rounded to x's
  * type for the two products that read it; grad_x gets back what the rounding of
- * its rows' targets took.
+ * its rows' targets took. float16 where the rows' upstream gradients differ (NONE
+ * or a z_weight): for grad_w a feature times its row's upstream gradient keeps all
+ * its bits down to 2^-27 of the largest such product, below it an absolute step.
  */
 apml_status apml_linear_ce_backward(const apml_linear_ce_desc *desc, const void *x, const void *w, const void *target,
                                     const float *state, const float *grad_loss, void *grad_x, void *grad_w,

@@ -61,6 +61,7 @@ struct CeBackwardPlan {
     bool whole_g;                // it holds float32 values as they are, else planes or 16-bit values
     bool sum_x;                  // grad_x is summed in float32 over several pieces or parts
     int tops;                    // workgroups of the pass over the upstream gradients (0: all rows have the same)
+    int size_lanes;              // lanes a row with which that pass reads x as well (0: it does not)
     size_t x, w, coef, block_top, top, xs, g, part_x, part_w, bytes;
 };
 CeBackwardPlan ce_plan_backward(const CeProblem &p, bool want_x, bool want_w);

@@ -637,8 +637,8 @@ struct FinishStats {
 struct CeCoef {
     float top, fac, at_target, unit;
 };
-// The units' common part, and the largest unit: every unit is the first times a
-// power of two.
+// The units' common part, and the one that w's gradient is summed in: every unit is
+// the first times a power of two.
 struct CeTop {
     float unit, top;
 };
@@ -978,34 +978,64 @@ struct Upstream {
     }
 };
 
-// The largest |b| over the rows that count, of upstream gradients b, and the
-// largest |b| + |c| with the penalty's part c = 2 z_weight lse b (5 us).
+// The largest |b| over the rows that count, of upstream gradients b, the largest
+// size |b| + |c| with the penalty's part c = 2 z_weight lse b, and the largest
+// size times a feature of its row.
+struct Largest {
+    float b, size, x;
+    __device__ __forceinline__ void join(const Largest &o)
+    {
+        b = fmaxf(b, o.b);
+        size = fmaxf(size, o.size);
+        x = fmaxf(x, o.x);
+    }
+    // over the workgroup, in its first thread (whole: in all of them)
+    __device__ __forceinline__ void join_all(Largest *sm, bool whole)
+    {
+        for (int o = 32; o > 0; o >>= 1)
+            join(Largest{__shfl_xor(b, o), __shfl_xor(size, o), __shfl_xor(x, o)});
+        if (lane_id() == 0)
+            sm[threadIdx.x >> 6] = *this;
+        __syncthreads();
+        if (whole || threadIdx.x == 0)
+            for (int w = 0; w < kBlock / 64; ++w)
+                join(sm[w]);
+    }
+};
+
+// FEATURES: with the float16 features x [n][dim], `lanes` lanes a row (1777 x
+// 1003: 5 us, 8192 x 1024: 9 us, 200000 x 64: 17 us), else one (5 us).
+template <bool FEATURES>
 __global__ __launch_bounds__(kBlock) void k_ce_size(const CeRow *rows, Targets target, Upstream up, float z_weight,
-                                                    int64_t n, float2 *block_top)
+                                                    int64_t n, const uint16_t *x, int dim, int lanes, Largest *block_top)
 {
-    __shared__ float2 sm[kBlock / 64];
-    float mb = 0.0f, ms = 0.0f;
-    for (int64_t i = (int64_t)blockIdx.x * kBlock + threadIdx.x; i < n; i += (int64_t)gridDim.x * kBlock) {
+    __shared__ Largest sm[kBlock / 64];
+    Largest m{0.0f, 0.0f, 0.0f};
+    const int per = FEATURES ? lanes : 1, lane = threadIdx.x & (per - 1);
+    for (int64_t i = ((int64_t)blockIdx.x * kBlock + threadIdx.x) / per; i < n; i += (int64_t)gridDim.x * (kBlock / per)) {
         const float b = up(i), size = fabsf(b) + (z_weight != 0.0f ? fabsf(2.0f * z_weight * rows[i].lse * b) : 0.0f);
-        if (target[i] != kIgnored && size < kInf) {
-            mb = fmaxf(mb, fabsf(b));
-            ms = fmaxf(ms, size);
+        if (target[i] == kIgnored || !(size < kInf))
+            continue;
+        float feature = 0.0f;
+        if constexpr (FEATURES) {
+            const uint16_t *row = x + i * dim;
+            for (int c = lane * 8; c < dim; c += per * 8) {
+                if (c + 8 <= dim) {
+                    const Loose<uint16_t, 8> v = *(const Loose<uint16_t, 8> *)(row + c);
+#pragma unroll
+                    for (int u = 0; u < 8; ++u)
+                        feature = fmaxf(feature, fabsf(F16::to(v.v[u])));
+                } else {
+                    for (int u = c; u < dim; ++u)
+                        feature = fmaxf(feature, fabsf(F16::to(row[u])));
+                }
+            }
         }
+        m.join(Largest{fabsf(b), size, fminf(feature * size, FLT_MAX)});
     }
-    for (int o = 32; o > 0; o >>= 1) {
-        mb = fmaxf(mb, __shfl_xor(mb, o));
-        ms = fmaxf(ms, __shfl_xor(ms, o));
-    }
-    if (lane_id() == 0)
-        sm[threadIdx.x >> 6] = make_float2(mb, ms);
-    __syncthreads();
-    if (threadIdx.x == 0) {
-        for (int w = 1; w < kBlock / 64; ++w) {
-            mb = fmaxf(mb, sm[w].x);
-            ms = fmaxf(ms, sm[w].y);
-        }
-        block_top[blockIdx.x] = make_float2(mb, ms);
-    }
+    m.join_all(sm, false);
+    if (threadIdx.x == 0)
+        block_top[blockIdx.x] = m;
 }
 
 // The smallest e with size <= unit 2^e, within [-60, 20].
@@ -1028,36 +1058,27 @@ struct Coefs {
     Targets target;
     Upstream up;
     float z_weight, stored_unit;
-    const float2 *block_top;
+    const Largest *block_top;
     int tops;
     // by the whole workgroup
     __device__ __forceinline__ CeTop top() const
     {
-        float mb, ms;
+        Largest m{0.0f, 0.0f, 0.0f};
         if (tops == 0) {
-            mb = ms = fabsf(up(0));
+            m.b = m.size = fabsf(up(0));
         } else {
-            __shared__ float2 sm[kBlock / 64];
-            mb = ms = 0.0f;
-            for (int i = threadIdx.x; i < tops; i += kBlock) {
-                mb = fmaxf(mb, block_top[i].x);
-                ms = fmaxf(ms, block_top[i].y);
-            }
-            for (int o = 32; o > 0; o >>= 1) {
-                mb = fmaxf(mb, __shfl_xor(mb, o));
-                ms = fmaxf(ms, __shfl_xor(ms, o));
-            }
-            if (lane_id() == 0)
-                sm[threadIdx.x >> 6] = make_float2(mb, ms);
-            __syncthreads();
-            for (int w = 0; w < kBlock / 64; ++w) {
-                mb = fmaxf(mb, sm[w].x);
-                ms = fmaxf(ms, sm[w].y);
-            }
+            __shared__ Largest sm[kBlock / 64];
+            for (int i = threadIdx.x; i < tops; i += kBlock)
+                m.join(block_top[i]);
+            m.join_all(sm, true);
         }
         // within 2^+-60: its smallest and largest multiples stay normal
-        const float unit = mb >= 0x1p-60f && mb <= 0x1p60f ? mb : 1.0f;
-        return CeTop{unit, ldexpf(unit, max(exponent_over(ms, unit), 0))};
+        const float unit = m.b >= 0x1p-60f && m.b <= 0x1p60f ? m.b : 1.0f;
+        const float top = ldexpf(unit, max(exponent_over(m.size, unit), 0));
+        // A row's unit is less than twice its size, so that its features times its
+        // unit over the one given here stay below 2^15 where m.x is known.
+        const int shift = m.x > 0.0f ? min(max(14 - exponent_over(m.x, top), 0), 40) : 0;
+        return CeTop{unit, ldexpf(top, -shift)};
     }
     __device__ __forceinline__ CeCoef operator()(int64_t i, const CeTop &t) const
     {
@@ -1079,9 +1100,11 @@ struct Coefs {
 };
 
 // Rows copied to dim_pad columns (zeros behind dim) and, where scaled, rows_out
-// rows a sample with every row times its unit over the largest one (a power of two:
-// no rounding but of float16 values below its normal range, an absolute step of
-// 2^-25 of the largest row's; zero for ignored rows, whatever they hold). In the backward
+// rows a sample with every row times its unit over that of w's gradient (a power of
+// two; zero for ignored rows, whatever they hold). Rows of equal weight stay as they
+// are; of others the largest product of a feature and its row's weight lies above
+// 2^13 in float16, so that features down to 2^-27 of it keep all their bits and
+// smaller ones are off by 2^-38 of it at most. In the backward
 // pass the first coef_blocks workgroups write the rows' coefficients. Bound by
 // memory (50001 x 1003 to 50001 x 1024 half precision, 203 MB: 45 us, 4.5 TB/s).
 template <class IN> __device__ __forceinline__ float get(const void *in, int64_t at) { return IN::to(((const uint16_t *)in)[at]); }
@@ -1750,6 +1773,15 @@ Cut cut_of(const CeProblem &p, const CeBackwardPlan &b, bool want_x, bool want_w
 
 } // namespace
 
+// Lanes that read a row of float16 features, 16 bytes each, of a wave.
+static int lanes_of(int dim)
+{
+    int lanes = 1;
+    while (lanes < 64 && lanes * 8 < dim)
+        lanes <<= 1;
+    return lanes;
+}
+
 CeBackwardPlan ce_plan_backward(const CeProblem &p, bool want_x, bool want_w)
 {
     CeBackwardPlan b{};
@@ -1783,8 +1815,10 @@ CeBackwardPlan ce_plan_backward(const CeProblem &p, bool want_x, bool want_w)
     b.x = o.take(b.pack_x ? n * b.dim_pad * size : 0);
     b.w = o.take(b.pack_w ? (int64_t)p.samples * p.classes * b.dim_pad * size : 0);
     b.coef = o.take(n * sizeof(CeCoef));
-    b.tops = p.reduction == 0 || p.z_weight != 0.0f ? (int)std::min<int64_t>(512, blocks_for(n, kBlock)) : 0;
-    b.block_top = o.take(b.tops * sizeof(float2));
+    const bool uneven = p.reduction == 0 || p.z_weight != 0.0f;
+    b.size_lanes = uneven && want_w && p.type == ElemType::f16 ? lanes_of(p.dim) : 0;
+    b.tops = uneven ? (int)std::min<int64_t>(512, blocks_for(n * std::max(b.size_lanes, 1), kBlock)) : 0;
+    b.block_top = o.take(b.tops * sizeof(Largest));
     b.top = o.take(sizeof(CeTop));
     b.xs = o.take(want_w ? (int64_t)p.samples * b.rows_pad * b.dim_pad * size : 0);
     b.g = o.take((int64_t)b.piece_samples * b.rows_pad * b.ld_g * size_g);
@@ -1802,7 +1836,7 @@ void ce_backward(const CeProblem &p, const CeBackwardPlan &plan, uint8_t *ws, co
 {
     const int64_t n = all_rows(p);
     auto *coef = (CeCoef *)(ws + plan.coef);
-    auto *block_top = (float2 *)(ws + plan.block_top);
+    auto *block_top = (Largest *)(ws + plan.block_top);
     auto *top = (CeTop *)(ws + plan.top);
     const Targets target = targets_of(p);
     const Upstream up{grad_loss, total, p.reduction, p.scale};
@@ -1815,8 +1849,12 @@ void ce_backward(const CeProblem &p, const CeBackwardPlan &plan, uint8_t *ws, co
         using IO = decltype(io);
         constexpr bool PLANES = decltype(cut)::value;
         const float inv_unit = 1.0f / ELEM::kUnit;
-        if (plan.tops)
-            k_ce_size<<<dim3(plan.tops), dim3(kBlock), 0, s>>>(rows, target, up, p.z_weight, n, block_top);
+        if (plan.tops && plan.size_lanes)
+            k_ce_size<true><<<dim3(plan.tops), dim3(kBlock), 0, s>>>(rows, target, up, p.z_weight, n, (const uint16_t *)p.x,
+                                                                     p.dim, plan.size_lanes, block_top);
+        else if (plan.tops)
+            k_ce_size<false><<<dim3(plan.tops), dim3(kBlock), 0, s>>>(rows, target, up, p.z_weight, n, nullptr, 0, 1,
+                                                                      block_top);
         Packs packs;
         packs.jobs.dim = p.dim;
         packs.jobs.dim_pad = plan.dim_pad;

@@ -593,3 +593,49 @@ def test_rows_of_no_weight_with_logits_far_below_zero(size, low, dtype):
             _, gx, gw = check(x, w, t, reduction=reduction, z_weight=z_weight, grad_loss=off)
             assert (gx == 0).all() and (gw == 0).all()
     check(x, w, t, z_weight=0.01)
+
+
+@pytest.mark.parametrize("dim", [64, 75, 600])
+@pytest.mark.parametrize("z_weight", [0.0, 1e-3])
+def test_float16_rows_of_small_weight_keep_their_bits_in_w(dim, z_weight):
+    """Half the rows weigh 2^-20 of the others and share no class with them, at upstream gradients under
+    which all results are in float16's normal range, as a scaled loss has them."""
+    gen = torch.Generator(device="cuda").manual_seed(9)
+    n = 32
+    x, w = torch.zeros(2 * n, dim, device="cuda"), torch.zeros(2 * n, dim, device="cuda")
+    x[:n, :n] = w[:n, :n] = 8.0 * torch.eye(n, device="cuda")  # sure of their classes: exp(-64) elsewhere
+    x[n:, n:] = torch.randn(n, dim - n, device="cuda", generator=gen)
+    w[n:, n:] = torch.randn(n, dim - n, device="cuda", generator=gen) * (2.0 / dim ** 0.5)
+    t = torch.cat([torch.arange(n, device="cuda"), torch.randint(n, 2 * n, (n,), device="cuda", generator=gen)])
+    up = torch.where(torch.arange(2 * n, device="cuda") < n, 2.0 ** 12, 2.0 ** -8)
+    x, w = x.half(), w.half()
+    _, _, gw = check(x, w, t, reduction="none", grad_loss=up, z_weight=z_weight)
+    X, W, T, U = x.double(), w.double(), t.unsqueeze(1), up.double().unsqueeze(1)
+    z = X @ W.T
+    lse = torch.logsumexp(z, 1, keepdim=True)
+    p = torch.softmax(z, 1)
+    one = torch.zeros_like(p).scatter(1, T, 1.0)
+    c = 1 + 2 * z_weight * lse
+    want = (U * (c * p - one)).T @ X
+    # an entry of the logits' gradient and the result are rounded once (2^-11), the logits' sums and the
+    # exponentials are off by 2^-15; a feature by 2^-38 of the largest one times its row's weight
+    size = U * (c * p * (1 - one) + (1 - p + 2 * z_weight * lse.abs()) * one)
+    largest = float((U * (1 + 2 * z_weight * lse.abs()) * X.abs()).max())
+    tol = size.T @ X.abs() * (2.0 ** -11 + 2.0 ** -14) + (size / U).sum(0).unsqueeze(1) * 2.0 ** -38 * largest
+    tol = tol + 2.0 ** -11 * want.abs() + 2.0 ** -24
+    oracle.within(gw[n:], want[n:], tol[n:], "grad_w")
+
+
+@pytest.mark.parametrize("weights", ["even", "uneven", "penalty"])
+def test_float16_features_next_to_the_largest(weights):
+    """The rows times their weights stay within the type."""
+    x, w, t = make(0, 40, 61, 64, F16)
+    x, w = x * 16000.0, w / 16000.0
+    x[3, 5] = 65504.0
+    up = torch.full(t.shape, 2.0 ** -9, device="cuda")
+    if weights == "uneven":
+        up = up * torch.logspace(-3, 0, 40, device="cuda")
+        up[3] = 2.0 ** -9
+    check(x, w, t, reduction="none", grad_loss=up, z_weight=0.1 if weights == "penalty" else 0.0)
+    x[:] = 0.0
+    check(x, w, t, reduction="none", grad_loss=up)
