@@ -13,8 +13,10 @@
 //
 // float32 operands are cut into three bfloat16 planes of 8 significant bits
 // each (exact: a = a0 + a1 + a2), and the product sums the six plane products
-// that reach 24 bits: a0 b0, a0 b1, a1 b0, a0 b2, a2 b0, a1 b1 (the rest is
-// below 2^-23 of a term). bfloat16 matrix instructions run at 16 times the rate
+// that reach 24 bits: a0 b0, a0 b1, a1 b0, a0 b2, a2 b0, a1 b1. Each plane is what is
+// left rounded to nearest, |a1| <= 2^-8 |a| and |a2| <= 2^-17 |a|, so that the rest is
+// at most 2^-24 of a term, as a rounding is, and of either sign (truncated planes
+// leave out up to 2^-21 and always towards 0, 2^-24.7 in the mean). bfloat16 matrix instructions run at 16 times the rate
 // of float32 ones, so six of them cost 3/8 of one float32 product.
 #include <algorithm>
 #include <cfloat>
@@ -94,18 +96,35 @@ struct F32 {
     }
 };
 
-// v cut into three bfloat16 values of 8 significant bits: v = a + b + c exactly
-// (truncated, so that no finite value becomes infinite).
+// v cut into three bfloat16 values of 8 significant bits, each the nearest to what
+// the ones before it leave: v = a + b + c exactly. ANY: also for values that round
+// to infinity (beyond 2^128 - 2^119; their first plane is truncated), which the
+// gradient of the logits, in units of the largest upstream gradient, does not have.
 struct Planes {
-    uint16_t a, b, c;
+    i16x8 a, b, c;
 };
-__device__ __forceinline__ Planes planes_of(float v)
+template <bool ANY> __device__ __forceinline__ Planes planes_of(const float (&v)[8])
 {
-    const uint32_t ua = __builtin_bit_cast(uint32_t, v) & 0xffff0000u;
-    const float r = v - __builtin_bit_cast(float, ua);
-    const uint32_t ub = __builtin_bit_cast(uint32_t, r) & 0xffff0000u;
-    const float q = r - __builtin_bit_cast(float, ub);
-    return {(uint16_t)(ua >> 16), (uint16_t)(ub >> 16), (uint16_t)(__builtin_bit_cast(uint32_t, q) >> 16)};
+    typedef float f32x2 __attribute__((ext_vector_type(2)));
+    typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+    i32x4 p[3];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) { // one conversion instruction a pair
+        f32x2 left = {v[2 * i], v[2 * i + 1]};
+#pragma unroll
+        for (int k = 0; k < 3; ++k) {
+            uint32_t w = __builtin_bit_cast(uint32_t, __builtin_convertvector(left, bf16x2));
+            if (ANY && k == 0) {
+                if ((w & 0x7fffu) == 0x7f80u)
+                    w = (w & 0xffff0000u) | __builtin_bit_cast(uint32_t, v[2 * i]) >> 16;
+                if ((w & 0x7fff0000u) == 0x7f800000u)
+                    w = (w & 0xffffu) | (__builtin_bit_cast(uint32_t, v[2 * i + 1]) & 0xffff0000u);
+            }
+            p[k][i] = (int)w;
+            left = left - f32x2{__builtin_bit_cast(float, w << 16), __builtin_bit_cast(float, w & 0xffff0000u)};
+        }
+    }
+    return {__builtin_bit_cast(i16x8, p[0]), __builtin_bit_cast(i16x8, p[1]), __builtin_bit_cast(i16x8, p[2])};
 }
 
 // The plane products of a float32 product.
@@ -276,13 +295,10 @@ __device__ __forceinline__ void float_fragment(const lds_char *tile, int r0, int
         for (int u = 0; u < 8; ++u)
             v[u] = *(const __attribute__((address_space(3))) float *)(at + u * (ROWS * 4));
     }
-#pragma unroll
-    for (int u = 0; u < 8; ++u) {
-        const Planes x = planes_of(v[u]);
-        planes[0][u] = (short)x.a;
-        planes[1][u] = (short)x.b;
-        planes[2][u] = (short)x.c;
-    }
+    const Planes x = planes_of<false>(v);
+    planes[0] = x.a;
+    planes[1] = x.b;
+    planes[2] = x.c;
 }
 
 // The tile shapes. A workgroup takes TP x TQ results, its waves WP x WQ of them,
@@ -720,14 +736,14 @@ template <Stored AS> struct FinishGrad {
             const int q0 = at.q0 + at.wq * (S::SQ * 16) + j * 16;
             const int64_t first = ((int64_t)at.sample * rows_pad + q0) * ld + w0;
             uint16_t *to = g + first;
-            const auto write = [&](auto value, uint16_t *out) {
+            const auto write = [&](auto values, uint16_t *out) {
 #pragma unroll
                 for (int k = 0; k < S::SP; k += 2) {
-                    i16x8 v;
+                    float v[8];
 #pragma unroll
                     for (int i = 0; i < 8; ++i)
-                        v[i] = (short)value(acc[k + (i >> 2)][j][i & 3]);
-                    *(lds_ptr<i16x8>)(at.lds + ((at.lane & 15) * LD + k * 16 + 8 * (at.lane >> 4)) * 2) = v;
+                        v[i] = acc[k + (i >> 2)][j][i & 3];
+                    *(lds_ptr<i16x8>)(at.lds + ((at.lane & 15) * LD + k * 16 + 8 * (at.lane >> 4)) * 2) = values(v);
                 }
                 wave_lds();
                 const int n = min(16, rows_pad - q0) * (W / 8);
@@ -756,11 +772,17 @@ template <Stored AS> struct FinishGrad {
                 }
                 wave_lds();
             } else if constexpr (AS == Stored::planes) {
-                write([](float v) { return planes_of(v).a; }, to);
-                write([](float v) { return planes_of(v).b; }, to + plane);
-                write([](float v) { return planes_of(v).c; }, to + 2 * plane);
+                write([](const float (&v)[8]) { return planes_of<false>(v).a; }, to);
+                write([](const float (&v)[8]) { return planes_of<false>(v).b; }, to + plane);
+                write([](const float (&v)[8]) { return planes_of<false>(v).c; }, to + 2 * plane);
             } else {
-                write([](float v) { return ELEM::from(v); }, to);
+                write([](const float (&v)[8]) {
+                    i16x8 r;
+#pragma unroll
+                    for (int i = 0; i < 8; ++i)
+                        r[i] = (short)ELEM::from(v[i]);
+                    return r;
+                }, to);
             }
             __builtin_amdgcn_sched_barrier(0); // rows side by side would not fit the registers
         }
@@ -1188,16 +1210,10 @@ template <class IN> __global__ __launch_bounds__(kBlock) void k_ce_pack(PackJobs
     }
     i16x8 p0;
     if constexpr (size == 4) {
-        i16x8 p1, p2;
-#pragma unroll
-        for (int u = 0; u < 8; ++u) {
-            const Planes x = planes_of(v[u]);
-            p0[u] = (short)x.a;
-            p1[u] = (short)x.b;
-            p2[u] = (short)x.c;
-        }
-        *(i16x8 *)(p.out + p.n + i) = p1;
-        *(i16x8 *)(p.out + 2 * p.n + i) = p2;
+        const Planes x = planes_of<true>(v);
+        p0 = x.a;
+        *(i16x8 *)(p.out + p.n + i) = x.b;
+        *(i16x8 *)(p.out + 2 * p.n + i) = x.c;
     } else {
 #pragma unroll
         for (int u = 0; u < 8; ++u)

@@ -639,3 +639,19 @@ def test_float16_features_next_to_the_largest(weights):
     check(x, w, t, reduction="none", grad_loss=up, z_weight=0.1 if weights == "penalty" else 0.0)
     x[:] = 0.0
     check(x, w, t, reduction="none", grad_loss=up)
+
+
+@pytest.mark.parametrize("rows,dim", [(4, 1), (4, 33), (130, 64), (130, 1000)])
+def test_float32_products_drop_less_than_a_rounding(rows, dim):
+    """c c for c = 1 + 2^-7 - 2^-23, whose last 16 bits are all ones: cut into 8-bit pieces that are
+    truncated, the pieces' products that are left out are 2^-21 of it."""
+    c = 1 + 2.0 ** -7 - 2.0 ** -23
+    x, w = torch.zeros(rows, dim, device="cuda"), torch.zeros(2, dim, device="cuda")
+    x[:, dim // 2] = c * torch.tensor([1.0, 2.0, 4.0, -8.0], device="cuda").repeat(rows)[:rows]
+    w[1, dim // 2] = c
+    t = (x[:, dim // 2] < 0).long()
+    # the loss is the larger logit, 16 c c and more, and log1p(exp(-16)) below 2^-23; float32: the scale in
+    # other units, the product's last sum, the result
+    loss = apml.linear_ce_loss(x, w, t, scale=16.0, reduction="none")
+    ref = oracle.linear_ce(x, w, t, scale=16.0, reduction="none")["loss"]
+    oracle.within(loss, ref, 3.25 * 2.0 ** -24 * ref, "loss")
