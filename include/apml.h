@@ -375,9 +375,9 @@ apml_status apml_linear_ce_forward(const apml_linear_ce_desc *desc, const void *
  * Gradients of sum grad_loss * loss: grad_loss device float32 [samples][rows]
  * (NONE) or one value; x, w, target and state as in the forward call. grad_x and
  * grad_w (shapes of x and w) are overwritten; one of them may be NULL. The logits'
- * gradient exists in pieces of the classes (or of the samples), rounded to x's
- * type for the two products that read it; grad_x gets back what the rounding of
- * its rows' targets took. float16 where the rows' upstream gradients differ (NONE
+ * gradient exists in pieces of 256 MB or less (of the samples, the classes, the
+ * rows), rounded to x's type for the two products that read it; grad_x gets back
+ * what the rounding of its rows' targets took. float16 where the rows' upstream gradients differ (NONE
  * or a z_weight): for grad_w a feature times its row's upstream gradient keeps all
  * its bits down to 2^-27 of the largest such product, below it an absolute step.
  */

@@ -55,11 +55,12 @@ void ce_forward(const CeProblem &p, const CeForwardPlan &plan, uint8_t *ws, floa
 struct CeBackwardPlan {
     bool pack_x, pack_w;
     int dim_pad, rows_pad;       // rows up to a multiple of kCeStep
-    int piece_samples, piece_classes; // the part of the logits' gradient that exists at a time
+    int piece_samples, piece_rows, piece_classes; // the part of the logits' gradient that exists at a time
+    int g_rows;                  // piece_rows up to a multiple of kCeStep
     int ld_g;                    // elements of a row of it, a multiple of kCeStep
     int split_x, split_w;        // parts of the sum over the classes (grad_x) and over the rows (grad_w)
     bool whole_g;                // it holds float32 values as they are, else planes or 16-bit values
-    bool sum_x;                  // grad_x is summed in float32 over several pieces or parts
+    bool sum_x, sum_w;           // the gradient is summed in float32 over several pieces or parts
     int tops;                    // workgroups of the pass over the upstream gradients (0: all rows have the same)
     int size_lanes;              // lanes a row with which that pass reads x as well (0: it does not)
     size_t x, w, coef, block_top, top, xs, g, part_x, part_w, bytes;

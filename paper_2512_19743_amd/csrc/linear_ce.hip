@@ -1775,6 +1775,11 @@ namespace {
 // a launch; 128 and 256 MB now: 32 x 2048 x 2048 x 64 float32 676 and 689 us, one
 // sample of 20000 x 20000 x 64 1895 and 1790).
 constexpr int64_t kPieceBytes = (int64_t)256 << 20;
+// A sample is cut along its classes, 256 at least; where its rows are too many for
+// that (524288 in 16 bits, 262144 or 174762 in float32) along its rows as well, into
+// pieces of about kCutClasses classes (600000 x 5000 x 256 bfloat16 9.8 ms, along the
+// classes alone 16.2; 200000 x 3000 x 128 float32 5.9 and 7.4).
+constexpr int64_t kLeastClasses = 256, kCutClasses = 2048;
 
 // Whether the logits' gradient is stored in float32 as it is, two thirds of its
 // planes: where the gradients' tile is ThinTriple.
@@ -1783,8 +1788,8 @@ bool whole_gradient(const CeProblem &p) { return p.type == ElemType::f32 && p.di
 // The gradients' launch of a whole piece.
 Cut cut_of(const CeProblem &p, const CeBackwardPlan &b, bool want_x, bool want_w)
 {
-    return choose_grads(p.dim, p.rows, b.piece_classes, b.piece_samples, ceil_to(b.piece_classes, kCeStep),
-                        b.rows_pad / kCeStep, planes(p), want_x, want_w);
+    return choose_grads(p.dim, b.piece_rows, b.piece_classes, b.piece_samples, ceil_to(b.piece_classes, kCeStep),
+                        b.g_rows / kCeStep, planes(p), want_x, want_w);
 }
 
 } // namespace
@@ -1806,17 +1811,26 @@ CeBackwardPlan ce_plan_backward(const CeProblem &p, bool want_x, bool want_w)
     b.rows_pad = (int)pad_to(p.rows, kCeStep);
     b.whole_g = whole_gradient(p);
     const int64_t n = all_rows(p), size = 2 * planes(p), size_g = b.whole_g ? 4 : size;
-    const int64_t whole = (int64_t)b.rows_pad * pad_to(p.classes, kCeStep) * size_g; // of one sample
+    const auto bytes_of = [&](int64_t rows, int64_t classes) { return pad_to(rows, kCeStep) * pad_to(classes, kCeStep) * size_g; };
+    b.piece_samples = 1;
+    b.piece_rows = p.rows;
+    b.piece_classes = p.classes;
+    const int64_t whole = bytes_of(p.rows, p.classes); // of one sample
     if (whole <= kPieceBytes) {
         const int pieces = ceil_to(p.samples, kPieceBytes / whole); // of about as many samples each
         b.piece_samples = ceil_to(p.samples, pieces);
-        b.piece_classes = p.classes;
     } else {
-        b.piece_samples = 1;
-        const int64_t most = std::max<int64_t>(256, kPieceBytes / (b.rows_pad * size_g) / 256 * 256);
-        const int pieces = ceil_to(p.classes, most);
-        b.piece_classes = (int)std::min<int64_t>(p.classes, pad_to(ceil_to(p.classes, pieces), 256));
+        if (bytes_of(p.rows, std::min<int64_t>(p.classes, kLeastClasses)) > kPieceBytes) {
+            const int64_t most = kPieceBytes / bytes_of(1, std::min<int64_t>(p.classes, kCutClasses)) * kCeStep / 256 * 256;
+            b.piece_rows = (int)std::min<int64_t>(p.rows, pad_to(ceil_to(p.rows, ceil_to(p.rows, most)), 256));
+        }
+        if (bytes_of(b.piece_rows, p.classes) > kPieceBytes) {
+            const int64_t most =
+                std::max(kLeastClasses, kPieceBytes / (pad_to(b.piece_rows, kCeStep) * size_g) / 256 * 256);
+            b.piece_classes = (int)std::min<int64_t>(p.classes, pad_to(ceil_to(p.classes, ceil_to(p.classes, most)), 256));
+        }
     }
+    b.g_rows = (int)pad_to(b.piece_rows, kCeStep);
     b.ld_g = (int)pad_to(b.piece_classes, kCeStep);
     // rows that lie a multiple of 2 KB apart share memory channels (16 x 4096 x
     // 16384 x 256: 3.42 ms, so 3.32; float32's three planes 0.89 and 0.90 ms)
@@ -1826,6 +1840,7 @@ CeBackwardPlan ce_plan_backward(const CeProblem &p, bool want_x, bool want_w)
     b.split_x = cut.split_x;
     b.split_w = cut.split_w;
     b.sum_x = b.split_x > 1 || b.piece_classes < p.classes;
+    b.sum_w = b.split_w > 1 || b.piece_rows < p.rows;
     const int64_t ld = pad_to(p.dim, 4);
     Offsets o;
     b.x = o.take(b.pack_x ? n * b.dim_pad * size : 0);
@@ -1837,9 +1852,11 @@ CeBackwardPlan ce_plan_backward(const CeProblem &p, bool want_x, bool want_w)
     b.block_top = o.take(b.tops * sizeof(Largest));
     b.top = o.take(sizeof(CeTop));
     b.xs = o.take(want_w ? (int64_t)p.samples * b.rows_pad * b.dim_pad * size : 0);
-    b.g = o.take((int64_t)b.piece_samples * b.rows_pad * b.ld_g * size_g);
-    b.part_x = o.take(want_x && b.sum_x ? (int64_t)b.split_x * b.piece_samples * p.rows * ld * 4 : 0);
-    b.part_w = o.take(want_w && b.split_w > 1 ? (int64_t)b.split_w * b.piece_samples * b.piece_classes * ld * 4 : 0);
+    b.g = o.take((int64_t)b.piece_samples * b.g_rows * b.ld_g * size_g);
+    // x's sums wait for all pieces of the classes, w's for a piece's rows alone
+    const int64_t part_rows = b.piece_classes < p.classes ? p.rows : b.piece_rows;
+    b.part_x = o.take(want_x && b.sum_x ? b.split_x * b.piece_samples * part_rows * ld * 4 : 0);
+    b.part_w = o.take(want_w && b.sum_w ? (int64_t)b.split_w * b.piece_samples * b.piece_classes * ld * 4 : 0);
     b.bytes = o.at;
     // alone a gradient may be cut into more parts: room for both is room for either
     if (want_x && want_w)
@@ -1894,102 +1911,102 @@ void ce_backward(const CeProblem &p, const CeBackwardPlan &plan, uint8_t *ws, co
         joins.jobs.ld = (int)ld;
         joins.jobs.top = top;
         joins.jobs.inv_unit = inv_unit;
-        for (int s0 = 0; s0 < p.samples; s0 += plan.piece_samples) {
-            const int ns = std::min(plan.piece_samples, p.samples - s0);
-            const TargetRest<IO> rest{target, (const uint16_t *)p.w + (int64_t)s0 * p.classes * p.dim,
-                                      coef + (int64_t)s0 * p.rows, (int64_t)s0 * p.rows, p.rows, p.dim, inv_unit};
+        // one piece after another: its samples from s0, classes from c0, rows from r0
+        const auto piece = [&](int s0, int c0, int r0) {
+            const int ns = std::min(plan.piece_samples, p.samples - s0); // more than one: with all classes and rows
+            const int nc = std::min(plan.piece_classes, p.classes - c0), nc_pad = (int)pad_to(nc, kCeStep);
+            const int nr = std::min(plan.piece_rows, p.rows - r0), nr_pad = (int)pad_to(nr, kCeStep);
+            const int64_t row0 = (int64_t)s0 * p.rows + r0;
+            const int64_t plane_g = (int64_t)plan.piece_samples * plan.g_rows * plan.ld_g;
+            const TargetRest<IO> rest{target, (const uint16_t *)p.w + (int64_t)s0 * p.classes * p.dim, coef + row0, row0,
+                                      nr, p.dim, inv_unit};
+            { // the logits again, and their gradient
+                Product a{};
+                a.p = W;
+                a.p.base += s0 * W.sample + (int64_t)c0 * W.ld;
+                a.p.rows = nc;
+                a.q = X;
+                a.q.base += s0 * X.sample + r0 * X.ld;
+                a.q.rows = nr;
+                a.steps = plan.dim_pad / kCeStep;
+                a.samples = ns;
+                a.splits = 1;
+                const auto product = [&](auto as) {
+                    launch_product<ELEM, PLANES>(choose(nc, nr, ns, false), a, nc_pad, nr_pad,
+                                                 FinishGrad<decltype(as)::value>{target, coef, row0, g, plane_g,
+                                                                                 scale2_of(p), nr_pad, plan.ld_g, c0}, s);
+                };
+                if constexpr (!PLANES)
+                    product(std::integral_constant<Stored, Stored::narrow>{});
+                else if (plan.whole_g)
+                    product(std::integral_constant<Stored, Stored::whole>{});
+                else
+                    product(std::integral_constant<Stored, Stored::planes>{});
+            }
+            Operand G;
+            G.base = g;
+            G.sample = (int64_t)nr_pad * plan.ld_g;
+            G.plane = plane_g;
+            G.ld = plan.ld_g;
+            if (plan.whole_g) { // in 16-bit elements
+                G.sample *= 2;
+                G.ld *= 2;
+            }
+            GradJob<IO> jx{}, jw{};
+            const bool cut_classes = nc < p.classes;
+            const int64_t sample_x = (int64_t)nr * ld, split_x = cut_classes ? p.rows * ld : ns * sample_x;
+            float *sum_x = part_x + (cut_classes ? r0 * ld : 0);
+            void *to_x = (uint8_t *)grad_x + row0 * p.dim * elem_size(p.type);
+            {
+                Product &a = jx.a;
+                a.p = W;
+                a.p.base += s0 * W.sample + (int64_t)c0 * W.ld;
+                a.p.rows = p.dim;
+                a.p.k = nc;
+                a.q = G;
+                a.q.rows = nr;
+                a.q.k = nc_pad;
+                a.steps = nc_pad / kCeStep;
+                a.samples = ns;
+                a.splits = plan.split_x;
+                jx.out.in_parts = plan.sum_x;
+                jx.out.part = FinishPart{sum_x, split_x, sample_x, (int)ld, c0 > 0};
+                jx.out.store = FinishStore<IO>{to_x, rest, coef + row0, top, inv_unit, (int64_t)p.rows * p.dim};
+            }
+            const int64_t sample_w = nc * ld, split_w = ns * sample_w, whole = (int64_t)p.classes * p.dim;
+            void *to_w = (uint8_t *)grad_w + (s0 * whole + (int64_t)c0 * p.dim) * elem_size(p.type);
+            {
+                Product &a = jw.a;
+                a.p.base = xs + ((int64_t)s0 * plan.rows_pad + r0) * plan.dim_pad;
+                a.p.sample = (int64_t)plan.rows_pad * plan.dim_pad;
+                a.p.plane = p.samples * a.p.sample;
+                a.p.ld = plan.dim_pad;
+                a.p.rows = p.dim;
+                a.p.k = nr_pad;
+                a.q = G;
+                a.q.rows = nc;
+                a.q.k = nr_pad;
+                a.steps = nr_pad / kCeStep;
+                a.samples = ns;
+                a.splits = plan.split_w;
+                jw.out.in_parts = plan.sum_w;
+                jw.out.part = FinishPart{part_w, split_w, sample_w, (int)ld, r0 > 0};
+                jw.out.store = FinishStore<IO>{to_w, rest, nullptr, top, inv_unit, whole};
+            }
+            launch_gradients<ELEM, PLANES>(cut_grads, jx, jw, grad_x, grad_w, s);
+            // what is complete is joined while its parts are in the cache and before
+            // the next piece writes over them
             joins.jobs.rest = rest;
-            for (int c0 = 0; c0 < p.classes; c0 += plan.piece_classes) {
-                const int nc = std::min(plan.piece_classes, p.classes - c0);
-                const int nc_pad = (int)pad_to(nc, kCeStep);
-                const int64_t plane_g = (int64_t)plan.piece_samples * plan.rows_pad * plan.ld_g;
-                { // the logits again, and their gradient
-                    Product a{};
-                    a.p = W;
-                    a.p.base += s0 * W.sample + (int64_t)c0 * W.ld;
-                    a.p.rows = nc;
-                    a.q = X;
-                    a.q.base += s0 * X.sample;
-                    a.steps = plan.dim_pad / kCeStep;
-                    a.samples = ns;
-                    a.splits = 1;
-                    const int64_t r0 = (int64_t)s0 * p.rows;
-                    const auto product = [&](auto as) {
-                        launch_product<ELEM, PLANES>(choose(nc, p.rows, ns, false), a, nc_pad, plan.rows_pad,
-                                                     FinishGrad<decltype(as)::value>{target, coef, r0, g, plane_g,
-                                                                                     scale2_of(p), plan.rows_pad,
-                                                                                     plan.ld_g, c0}, s);
-                    };
-                    if constexpr (!PLANES)
-                        product(std::integral_constant<Stored, Stored::narrow>{});
-                    else if (plan.whole_g)
-                        product(std::integral_constant<Stored, Stored::whole>{});
-                    else
-                        product(std::integral_constant<Stored, Stored::planes>{});
-                }
-                Operand G;
-                G.base = g;
-                G.sample = (int64_t)plan.rows_pad * plan.ld_g;
-                G.plane = plane_g;
-                G.ld = plan.ld_g;
-                if (plan.whole_g) { // in 16-bit elements
-                    G.sample *= 2;
-                    G.ld *= 2;
-                }
-                GradJob<IO> jx{}, jw{};
-                {
-                    Product &a = jx.a;
-                    a.p = W;
-                    a.p.base += s0 * W.sample + (int64_t)c0 * W.ld;
-                    a.p.rows = p.dim;
-                    a.p.k = nc;
-                    a.q = G;
-                    a.q.rows = p.rows;
-                    a.q.k = nc_pad;
-                    a.steps = nc_pad / kCeStep;
-                    a.samples = ns;
-                    a.splits = plan.split_x;
-                    const int64_t part = (int64_t)p.rows * ld, whole = (int64_t)p.rows * p.dim;
-                    jx.out.in_parts = plan.sum_x;
-                    jx.out.part = FinishPart{part_x, plan.piece_samples * part, part, (int)ld, c0 > 0};
-                    jx.out.store = FinishStore<IO>{(uint8_t *)grad_x + s0 * whole * elem_size(p.type), rest,
-                                                   coef + (int64_t)s0 * p.rows, top, inv_unit, whole};
-                }
-                const int64_t part = (int64_t)nc * ld, whole = (int64_t)p.classes * p.dim;
-                void *to = (uint8_t *)grad_w + (s0 * whole + (int64_t)c0 * p.dim) * elem_size(p.type);
-                {
-                    Product &a = jw.a;
-                    a.p.base = xs + (int64_t)s0 * plan.rows_pad * plan.dim_pad;
-                    a.p.sample = (int64_t)plan.rows_pad * plan.dim_pad;
-                    a.p.plane = p.samples * a.p.sample;
-                    a.p.ld = plan.dim_pad;
-                    a.p.rows = p.dim;
-                    a.p.k = plan.rows_pad;
-                    a.q = G;
-                    a.q.rows = nc;
-                    a.q.k = plan.rows_pad;
-                    a.steps = plan.rows_pad / kCeStep;
-                    a.samples = ns;
-                    a.splits = plan.split_w;
-                    jw.out.in_parts = plan.split_w > 1;
-                    jw.out.part = FinishPart{part_w, ns * part, part, (int)ld, false};
-                    jw.out.store = FinishStore<IO>{to, rest, nullptr, top, inv_unit, whole};
-                }
-                launch_gradients<ELEM, PLANES>(cut_grads, jx, jw, grad_x, grad_w, s);
-                if (grad_w && plan.split_w > 1) {
-                    // several samples only where a piece holds all their classes
-                    joins.add(part_w, to, (int64_t)ns * nc, ns * part, plan.split_w, nullptr);
-                    if (c0 + plan.piece_classes < p.classes)
-                        joins.launch(s); // before its parts are written over
-                }
-            }
-            if (grad_x && plan.sum_x) {
-                const int64_t sample = (int64_t)p.rows * ld, split = plan.piece_samples * sample;
-                joins.add(part_x, (uint8_t *)grad_x + (int64_t)s0 * p.rows * p.dim * elem_size(p.type),
-                          (int64_t)ns * p.rows, split, plan.split_x, coef + (int64_t)s0 * p.rows);
-            }
-            joins.launch(s); // while its parts are in the cache
-        }
+            if (grad_w && plan.sum_w && r0 + nr == p.rows)
+                joins.add(part_w, to_w, (int64_t)ns * nc, split_w, plan.split_w, nullptr);
+            if (grad_x && plan.sum_x && c0 + nc == p.classes)
+                joins.add(sum_x, to_x, (int64_t)ns * nr, split_x, plan.split_x, coef + row0);
+            joins.launch(s);
+        };
+        for (int s0 = 0; s0 < p.samples; s0 += plan.piece_samples)
+            for (int c0 = 0; c0 < p.classes; c0 += plan.piece_classes)
+                for (int r0 = 0; r0 < p.rows; r0 += plan.piece_rows)
+                    piece(s0, c0, r0);
     });
 }
 

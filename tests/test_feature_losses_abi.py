@@ -159,3 +159,24 @@ def test_results_off_their_elements_are_refused():
     for state, g in ((ODD, FAKE), (FAKE, ODD)):
         assert lib.apml_balance_backward(ctypes.byref(b), FAKE, None, state, g, FAKE, None) == 1
     assert lib.apml_expert_counts(FAKE, 0, None, 1, 8, 2, 4, ctypes.c_void_p(FAKE.value + 4), None) == 1
+
+
+@pytest.mark.parametrize("kw", [dict(dtype=1, rows=1 << 20, classes=40), dict(dtype=1, rows=1 << 22, classes=300),
+                                dict(dtype=2, rows=1 << 26, classes=13), dict(dtype=0, rows=1 << 22, classes=300, dim=72),
+                                dict(dtype=0, rows=1 << 21, classes=5000, dim=64), dict(dtype=1, rows=1 << 20, classes=1 << 17),
+                                dict(dtype=1, samples=4, rows=1 << 20, classes=700), dict(dtype=1, rows=524289, classes=256),
+                                dict(dtype=0, rows=8192, classes=131072, dim=1024), dict(dtype=1, samples=4096, rows=300, classes=300)],
+                         ids=str)
+def test_backward_workspace_keeps_to_its_piece(kw):
+    """Beside copies of x and w, the rows' coefficients and sums of gradients in float32, all of the
+    inputs' size, the backward pass has a piece of the logits' gradient of 256 MB (rows up to 192
+    elements longer than the piece) at any sizes."""
+    lib, d, n = _lib.load(), ce_desc(**{"dim": 64, **kw}), ctypes.c_size_t()
+    assert lib.apml_linear_ce_workspace(ctypes.byref(d), FAKE, FAKE, None, ctypes.byref(n)) == 0
+    up = lambda a: (a + 63) // 64 * 64  # noqa: E731
+    size, dim = (6 if d.dtype == 0 else 2), up(d.dim)
+    rows, classes = d.samples * up(d.rows), d.samples * d.classes
+    copies = (2 * rows * dim + classes * dim) * size + 16 * rows
+    sums = 4 * (rows + 2 * classes) * dim  # one for x's, two parts for w's
+    parts = 64 << 20  # of small gradients, up to 64 each
+    assert n.value <= copies + sums + parts + 1.2 * (256 << 20)

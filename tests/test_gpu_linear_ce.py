@@ -655,3 +655,20 @@ def test_float32_products_drop_less_than_a_rounding(rows, dim):
     loss = apml.linear_ce_loss(x, w, t, scale=16.0, reduction="none")
     ref = oracle.linear_ce(x, w, t, scale=16.0, reduction="none")["loss"]
     oracle.within(loss, ref, 3.25 * 2.0 ** -24 * ref, "loss")
+
+
+@pytest.mark.parametrize("size,dtype", [((0, 530000, 300, 40), BF16), ((0, 530001, 270, 72), F16),
+                                        ((0, 175000, 2600, 72), F32), ((0, 263001, 260, 24), F32),
+                                        ((0, 2200000, 40, 8), BF16), ((2, 264000, 257, 16), F32)],
+                         ids=lambda v: "x".join(map(str, v)) if isinstance(v, tuple) else str(v)[6:])
+def test_pieces_of_the_rows(size, dtype):
+    """So many rows that a piece of all of them would be too large at the fewest classes."""
+    x, w, t = make(*size, dtype, ignored=0.1)
+    up = torch.full((), 2.0 ** -6, device="cuda")
+    _, gx, gw = check(x, w, t, reduction="sum", z_weight=1e-3, grad_loss=up)
+    _, state = apml.apml_linear_ce_forward(x, w, t, reduction="sum", z_weight=1e-3)
+    alone = dict(reduction="sum", z_weight=1e-3)
+    a, none = apml.apml_linear_ce_backward(state, x, w, t, up, want_grad_w=False, **alone)
+    assert none is None and (a.double() - gx.double()).abs().max() <= 2.0 ** -7 * gx.double().abs().max()
+    none, b = apml.apml_linear_ce_backward(state, x, w, t, up, want_grad_x=False, **alone)
+    assert none is None and (b.double() - gw.double()).abs().max() <= 2.0 ** -7 * gw.double().abs().max()
