@@ -196,14 +196,21 @@ struct BalanceArgs {
     int *ticket;   // cleared for k_balance_join
 };
 
+// Tokens that a lane group adds up in float32 before its sums go into the chunk's, in
+// double precision: equal addends, whose roundings all go one way, are off by half
+// as many half steps at most (524288 equal tokens of 2 experts, 4096 a group, in one
+// float32 sum: 5e-5 off). Both took the same time where a chunk is one run (16 x 8192
+// x 64: 13.2 us).
+constexpr int kRunTokens = 128;
+
 // A chunk's sums of the probabilities, its tokens per expert and its sum of lse^2.
 // Bound by the latency of few rows a lane group (16 x 8192 tokens of 64 experts in
 // bfloat16, 17 MB: 14 us) and, for rows of odd length, by the exponentials.
 template <class L, int VEC, int NV>
 __global__ __launch_bounds__(kBlock) void k_balance_chunks(BalanceArgs a, bool index32)
 {
-    extern __shared__ __attribute__((aligned(16))) float sm[]; // [E] sums, then [E] counts
-    __shared__ float sz[kBlock / 64];
+    extern __shared__ __attribute__((aligned(16))) double sm[]; // [E] sums, then [E] counts
+    __shared__ double sz[kBlock / 64];
     __shared__ int sn[kBlock / 64];
     int *hist = (int *)(sm + a.E);
     const int sample = blockIdx.x / a.chunks, chunk = blockIdx.x % a.chunks;
@@ -212,7 +219,7 @@ __global__ __launch_bounds__(kBlock) void k_balance_chunks(BalanceArgs a, bool i
     if (blockIdx.x == 0 && threadIdx.x == 0)
         *a.ticket = 0;
     for (int e = threadIdx.x; e < a.E; e += kBlock) {
-        sm[e] = 0.0f;
+        sm[e] = 0.0;
         hist[e] = 0;
     }
     __syncthreads();
@@ -223,12 +230,10 @@ __global__ __launch_bounds__(kBlock) void k_balance_chunks(BalanceArgs a, bool i
         else
             count_chunk<false>(a.index, a.valid, row0 + t0, t1 - t0, a.chosen, a.E, hist, kBlock);
     }
-    float acc[NV * VEC];
-#pragma unroll
-    for (int i = 0; i < NV * VEC; ++i)
-        acc[i] = 0.0f;
-    float z = 0.0f;
+    float acc[NV * VEC], z = 0.0f;
+    double zs = 0.0;
     int n = 0;
+    const int wave = threadIdx.x >> 6, in_wave = threadIdx.x & 63;
     const auto add = [&](float (&v)[NV * VEC]) {
         float inv;
         const float lse = exp_row(v, a.lanes, &inv);
@@ -238,75 +243,84 @@ __global__ __launch_bounds__(kBlock) void k_balance_chunks(BalanceArgs a, bool i
         z = __builtin_fmaf(lse, lse, z);
         ++n;
     };
-    if constexpr (VEC > 1) {
-        for (int t = t0 + group; t < t1; t += 2 * groups) { // two rows' loads in flight
-            const int64_t r = row0 + t, q = r + groups;
-            const bool two = t + groups < t1;
-            const bool vr = !a.valid || a.valid[r], vq = two && (!a.valid || a.valid[q]);
-            float v[NV * VEC], w[NV * VEC];
-            load_row<L, VEC, NV>((const typename L::raw *)a.logits + r * a.E, lane, a.lanes, a.E, v);
-            load_row<L, VEC, NV>((const typename L::raw *)a.logits + (two ? q : r) * a.E, lane, a.lanes, a.E, w);
-            if (vr)
-                add(v);
-            if (vq)
-                add(w);
-        }
-    } else {
-        using R = typename L::raw;
-        R *lds = (R *)(sm + ((2 * a.E + 3) & ~3));
-        for (int b = t0; b < t1; b += a.tile) {
-            const int n_tok = min(a.tile, t1 - b);
-            __syncthreads();
-            const R *rows = tile_in(lds, (const R *)a.logits + (row0 + b) * a.E, n_tok * a.E);
-            __syncthreads();
-            for (int t = group; t < n_tok; t += groups) {
-                if (a.valid && !a.valid[row0 + b + t])
-                    continue;
-                float v[NV * VEC];
-                load_row<L, VEC, NV>(rows + t * a.E, lane, a.lanes, a.E, v);
-                add(v);
-            }
-        }
-    }
-    // the groups of a wave, then the waves one after another: a fixed order
-    for (int o = a.lanes; o < 64; o <<= 1) {
+    for (int r0 = t0; r0 < t1; r0 += groups * kRunTokens) {
+        const int r1 = min(r0 + groups * kRunTokens, t1);
 #pragma unroll
         for (int i = 0; i < NV * VEC; ++i)
-            acc[i] += __shfl_xor(acc[i], o);
-        z += __shfl_xor(z, o);
+            acc[i] = 0.0f;
+        if constexpr (VEC > 1) {
+            for (int t = r0 + group; t < r1; t += 2 * groups) { // two rows' loads in flight
+                const int64_t r = row0 + t, q = r + groups;
+                const bool two = t + groups < r1;
+                const bool vr = !a.valid || a.valid[r], vq = two && (!a.valid || a.valid[q]);
+                float v[NV * VEC], w[NV * VEC];
+                load_row<L, VEC, NV>((const typename L::raw *)a.logits + r * a.E, lane, a.lanes, a.E, v);
+                load_row<L, VEC, NV>((const typename L::raw *)a.logits + (two ? q : r) * a.E, lane, a.lanes, a.E, w);
+                if (vr)
+                    add(v);
+                if (vq)
+                    add(w);
+            }
+        } else {
+            using R = typename L::raw;
+            R *lds = (R *)((float *)sm + ((3 * a.E + 3) & ~3));
+            for (int b = r0; b < r1; b += a.tile) {
+                const int n_tok = min(a.tile, r1 - b);
+                __syncthreads();
+                const R *rows = tile_in(lds, (const R *)a.logits + (row0 + b) * a.E, n_tok * a.E);
+                __syncthreads();
+                for (int t = group; t < n_tok; t += groups) {
+                    if (a.valid && !a.valid[row0 + b + t])
+                        continue;
+                    float v[NV * VEC];
+                    load_row<L, VEC, NV>(rows + t * a.E, lane, a.lanes, a.E, v);
+                    add(v);
+                }
+            }
+        }
+        // the groups of a wave, then the waves one after another: a fixed order
+        for (int o = a.lanes; o < 64; o <<= 1) {
+#pragma unroll
+            for (int i = 0; i < NV * VEC; ++i)
+                acc[i] += __shfl_xor(acc[i], o);
+        }
+        for (int w = 0; w < kBlock / 64; ++w) {
+            if (wave == w && in_wave < a.lanes) {
+#pragma unroll
+                for (int i = 0; i < NV; ++i)
+#pragma unroll
+                    for (int u = 0; u < VEC; ++u) {
+                        const int c = (i * a.lanes + lane) * VEC + u;
+                        if (c < a.E)
+                            sm[c] += (double)acc[i * VEC + u];
+                    }
+            }
+            __syncthreads();
+        }
+        zs += (double)z;
+        z = 0.0f;
+    }
+    for (int o = a.lanes; o < 64; o <<= 1) {
+        zs += __shfl_xor(zs, o);
         n += __shfl_xor(n, o);
     }
-    const int wave = threadIdx.x >> 6, in_wave = threadIdx.x & 63;
-    for (int w = 0; w < kBlock / 64; ++w) {
-        if (wave == w && in_wave < a.lanes) {
-#pragma unroll
-            for (int i = 0; i < NV; ++i)
-#pragma unroll
-                for (int u = 0; u < VEC; ++u) {
-                    const int c = (i * a.lanes + lane) * VEC + u;
-                    if (c < a.E)
-                        sm[c] += acc[i * VEC + u];
-                }
-        }
-        __syncthreads();
-    }
     if (in_wave == 0) {
-        sz[wave] = z;
+        sz[wave] = zs;
         sn[wave] = n;
     }
     __syncthreads();
     const int64_t at = (int64_t)blockIdx.x * a.E;
     for (int e = threadIdx.x; e < a.E; e += kBlock) {
-        a.p[at + e] = sm[e];
+        a.p[at + e] = (float)sm[e];
         if (a.index)
             a.count[at + e] = hist[e];
     }
     if (threadIdx.x == 0) {
         for (int w = 1; w < kBlock / 64; ++w) {
-            z += sz[w];
+            zs += sz[w];
             n += sn[w];
         }
-        a.z[blockIdx.x] = ChunkSum{z, n};
+        a.z[blockIdx.x] = ChunkSum{(float)zs, n};
     }
 }
 
@@ -491,7 +505,7 @@ __global__ __launch_bounds__(kBlock) void k_balance_grad(BalanceArgs a, const fl
                 finish(w, vq, (typename L::raw *)out + q * a.E);
         }
     } else {
-        extern __shared__ __attribute__((aligned(16))) float sm[];
+        extern __shared__ __attribute__((aligned(16))) double sm[];
         using R = typename L::raw;
         R *lds = (R *)sm;
         for (int b = t0; b < t1; b += a.tile) {
@@ -658,7 +672,7 @@ void balance_forward(const BalanceProblem &p, const BalancePlan &plan, uint8_t *
     by_shape(p.type, r, [&](auto l, auto vec, auto nv) {
         k_balance_chunks<decltype(l), decltype(vec)::value, decltype(nv)::value>
             <<<dim3((unsigned)(p.samples * a.chunks)), dim3(kBlock),
-               ((2 * p.experts + 3) & ~3) * sizeof(float) + tile_bytes(p, r), s>>>(a, p.index32);
+               ((3 * p.experts + 3) & ~3) * sizeof(float) + tile_bytes(p, r), s>>>(a, p.index32);
     });
     k_balance_join<<<dim3(p.samples), dim3(1024), 0, s>>>(a, counts, loss, state, p.reduction, (float *)(ws + plan.loss),
                                                          a.ticket);

@@ -351,3 +351,25 @@ def test_shares_that_are_nearly_equal(experts, slots_dropped):
     assert ((got - g * p * (d - dot)).abs() <= tol).all()
     if slots_dropped == 0.0:
         assert (counts == counts[:, :1]).all() and not got.any()
+
+
+@pytest.mark.parametrize("experts,tokens,dtype,low", [(2, 524288, F16, -1.375), (2, 524288, F16, 2.25),
+                                                      (8, 262144, BF16, -1.375), (4, 262144, F32, 2.25)],
+                         ids=["2 f16", "2 f16 other", "8 bf16", "4 f32"])
+def test_long_samples_of_equal_tokens(experts, tokens, dtype, low):
+    """1024 samples, each a chunk of its own, whose tokens add the same number to a sum again and again."""
+    row = torch.zeros(experts, device="cuda", dtype=dtype)
+    row[0] = low
+    logits = row.expand(1024, tokens, experts).contiguous()
+    counts = torch.zeros(1024, experts, device="cuda", dtype=torch.int64)
+    counts[:, 0] = 7
+    z = row.double()
+    want = experts * torch.softmax(z, 0)[0]
+    # at most 128 such sums in float32, off by half as many half steps of the last; the exponentials,
+    # the softmax's sum and quotient 2^-20
+    rel = 64 * 2.0 ** -24 + 2.0 ** -20
+    loss, _ = apml.balance_loss(logits, counts=counts, reduction="none")
+    oracle.within(loss, want.expand(1024), want.expand(1024) * rel, "loss")
+    loss, _ = apml.balance_loss(logits, counts=counts, reduction="none", z_weight=1.0)
+    want = want + torch.logsumexp(z, 0).square()
+    oracle.within(loss, want.expand(1024), want.expand(1024) * (rel + 2.0 ** -20), "loss")
