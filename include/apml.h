@@ -345,7 +345,7 @@ typedef struct apml_linear_ce_desc {
     int32_t classes;      /* >= 1, <= 2^26 */
     int32_t dim;          /* >= 1, <= 2^20; some 2^38 logits, or 2^35 features of either side, a call */
     int32_t reduction;    /* apml_reduction */
-    float scale;          /* 1 / temperature */
+    float scale;          /* 1 / temperature; within +-2.35e38 */
     float z_weight;       /* weight of lse^2 */
     int64_t ignore_index;
 } apml_linear_ce_desc;

@@ -14,6 +14,7 @@ enum class ElemType : int { f32 = 0, bf16 = 1, f16 = 2 };
 inline size_t elem_size(ElemType t) { return t == ElemType::f32 ? 4 : 2; }
 
 constexpr int kCeStep = 64; // elements of the summed axis that one step of a product takes
+constexpr float kLog2E = 1.44269504088896340736f;
 
 // What the forward pass keeps of a row: its largest logit in units of log 2,
 // 1 / sum exp(z - top), the part of its softmax that is not the target's, and its

@@ -38,8 +38,6 @@ typedef short i16x8 __attribute__((ext_vector_type(8)));
 
 using lds_char = __attribute__((address_space(3))) char;
 
-constexpr float kLog2E = 1.44269504088896340736f;
-
 // The rows' targets as the caller holds them.
 constexpr int kIgnored = -1, kOutside = -2;
 struct Targets {

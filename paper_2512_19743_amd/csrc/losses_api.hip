@@ -46,6 +46,8 @@ apml_status check_desc(const apml_linear_ce_desc *d)
         return bad("need samples >= 1, rows >= 1, classes >= 1 and dim >= 1");
     if (!std::isfinite(d->scale) || !std::isfinite(d->z_weight))
         return bad("scale and z_weight must be finite");
+    if (!std::isfinite(d->scale * kLog2E)) // what the logits are multiplied by
+        return bad("scale must lie within +-2.35e38");
     // a launch's workgroups and the offsets within a tile are 32-bit
     if (d->dim > (1 << 20) || d->classes > (1 << 26) || (int64_t)d->samples * d->rows > (1 << 26))
         return fail_with(APML_ERR_UNSUPPORTED, "dim beyond 2^20, classes beyond 2^26 or samples * rows beyond 2^26");

@@ -180,3 +180,15 @@ def test_backward_workspace_keeps_to_its_piece(kw):
     sums = 4 * (rows + 2 * classes) * dim  # one for x's, two parts for w's
     parts = 64 << 20  # of small gradients, up to 64 each
     assert n.value <= copies + sums + parts + 1.2 * (256 << 20)
+
+
+@pytest.mark.parametrize("scale,status", [(3e38, 1), (-3e38, 1), (2.3e38, 0), (-2.3e38, 0)])
+def test_a_scale_beyond_float32_in_units_of_log_2_is_refused(scale, status):
+    """The kernels multiply by scale / log 2, which would be infinite: NaN for a logit of 0."""
+    lib, d, n = _lib.load(), ce_desc(scale=scale), ctypes.c_size_t()
+    assert lib.apml_linear_ce_workspace(ctypes.byref(d), None, None, ctypes.byref(n), None) == status
+    if status:
+        assert lib.apml_linear_ce_forward(ctypes.byref(d), FAKE, FAKE, FAKE, FAKE, FAKE, FAKE, 1 << 60, None) == status
+        assert lib.apml_linear_ce_backward(ctypes.byref(d), FAKE, FAKE, FAKE, FAKE, FAKE, FAKE, FAKE, FAKE, 1 << 60,
+                                           None) == status
+        assert "scale" in lib.apml_last_error().decode()
