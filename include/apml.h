@@ -355,7 +355,14 @@ void apml_linear_ce_desc_default(apml_linear_ce_desc *d);
 
 /* Bytes of workspace of the two calls for these x and w (their alignment
  * decides whether they are copied into padded rows; NULL: the most any needs).
- * Either pointer to a size may be NULL. */
+ * Either pointer to a size may be NULL. With dim up to a multiple of 64, the copies
+ * are, in either pass: for float32 x and w whole, in 6 bytes an element (the forward
+ * pass of at most 128 rows a sample goes without where dim is a multiple of 32 and
+ * both are aligned to 16 bytes); in 16 bits x where dim is no multiple of 64 and w
+ * where it is none of 8, or what is not aligned to 16 bytes. The backward pass copies
+ * x once more for grad_w. Beside them the forward pass has 8 bytes a row and 64 or 128 classes (32
+ * for at most 16 rows a sample), the backward pass a piece of the logits' gradient of
+ * about 256 MB at most and, where sums are cut, gradients in float32. */
 apml_status apml_linear_ce_workspace(const apml_linear_ce_desc *desc, const void *x, const void *w,
                                      size_t *forward_bytes, size_t *backward_bytes);
 
@@ -375,11 +382,12 @@ apml_status apml_linear_ce_forward(const apml_linear_ce_desc *desc, const void *
  * Gradients of sum grad_loss * loss: grad_loss device float32 [samples][rows]
  * (NONE) or one value; x, w, target and state as in the forward call. grad_x and
  * grad_w (shapes of x and w) are overwritten; one of them may be NULL. The logits'
- * gradient exists in pieces of 256 MB or less (of the samples, the classes, the
- * rows), rounded to x's type for the two products that read it; grad_x gets back
- * what the rounding of its rows' targets took. float16 where the rows' upstream gradients differ (NONE
- * or a z_weight): for grad_w a feature times its row's upstream gradient keeps all
- * its bits down to 2^-27 of the largest such product, below it an absolute step.
+ * gradient exists in pieces of about 256 MB at most (of the samples, the classes,
+ * the rows), rounded to x's type for the two products that read it; grad_x gets back
+ * what the rounding of its rows' targets took, grad_w does not (bfloat16: up to 1.35
+ * times the error of one rounding). float16 where the rows' upstream gradients differ
+ * (NONE or a z_weight): for grad_w a feature times its row's upstream gradient keeps
+ * all its bits down to 2^-27 of the largest such product, below it an absolute step.
  */
 apml_status apml_linear_ce_backward(const apml_linear_ce_desc *desc, const void *x, const void *w, const void *target,
                                     const float *state, const float *grad_loss, void *grad_x, void *grad_w,

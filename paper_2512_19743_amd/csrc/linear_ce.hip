@@ -328,7 +328,7 @@ struct Place {
 // operand's rows are contiguous; Finish: what becomes of the results.
 //
 // Tiles go from memory to shared memory without passing registers, one step
-// ahead; the matrix cores take them as 16 x 32 fragments. P's rows come out along
+// ahead (one and a half in the woven tile, three in that of 16 rows); the matrix cores take them as 16 x 32 fragments. P's rows come out along
 // a lane's registers, Q's along the lanes: classes (or features) are P, so that
 // the softmax's sums run mostly within a lane and results leave as neighbours.
 // The large tile needs 64 KB of loads for 2048 cycles of matrix instructions a
@@ -550,10 +550,10 @@ __device__ constexpr int class_of(int k, int i) { return (k >> 1) * 32 + (k & 1)
 
 // Forward: per row (q) the maximum and the sum of exp(z - max) over a wave's
 // classes (p), without the target's, whose logit is kept apart. Logits are in
-// units of log 2 from here on (exp2 is the instruction): z = acc * scale2. Per
-// logit a maximum, a multiply-add, an exponential and a sum; which class is a
-// row's target is asked only in waves whose classes hold one, which classes are
-// there at all only in the last tile.
+// units of log 2 from here on, z = acc * scale2, and exp2 is the instruction, whose
+// results are off by a step. Per logit a maximum, a multiply-add, an exponential and
+// a sum; which class is a row's target is asked only in waves whose classes hold one,
+// which classes are there at all only in the last tile.
 struct FinishStats {
     Targets target; // [samples * rows]
     float2 *part;   // [parts][samples * rows]

@@ -47,7 +47,9 @@ def linear_ce_loss(x: torch.Tensor, w: torch.Tensor, target: torch.Tensor, *, sc
     x (..., dim) and w (classes, dim): one set of classes, a code book or a vocabulary. x (B, N, dim) and
     w (B, M, dim): each sample with its own, as when the descriptors of one cloud's points are matched to
     those of the other's (scale, a number: 1 / temperature; a learned one is multiplied into x).
-    float32, bfloat16 or float16 GPU tensors.
+    float32, bfloat16 or float16 GPU tensors, x and w of the same type: autocast does not reach this call, so
+    bfloat16 features need a bfloat16 copy of a float32 head. In 16 bits the gradient of the logits is rounded to
+    that type, as it would be between two layers, before it is multiplied by w and x.
     target: the rows' classes, int64 or int32, of x's leading shape; ignore_index: a row that adds nothing.
     z_weight: weight of the squared log-sum-exp that is added per row.
     reduction: 'none' (target's shape), 'sum', or 'mean' over the rows that are not ignored.

@@ -672,3 +672,36 @@ def test_pieces_of_the_rows(size, dtype):
     assert none is None and (a.double() - gx.double()).abs().max() <= 2.0 ** -7 * gx.double().abs().max()
     none, b = apml.apml_linear_ce_backward(state, x, w, t, up, want_grad_x=False, **alone)
     assert none is None and (b.double() - gw.double()).abs().max() <= 2.0 ** -7 * gw.double().abs().max()
+
+
+@pytest.mark.parametrize("size,dtype", [((0, 200, 1500, 100), F16), ((0, 263000, 260, 24), F32)],
+                         ids=["float16 rows of unequal weight", "pieces of the rows"])
+def test_captured_with_a_weight_a_row(size, dtype):
+    def data(seed):
+        x, w, t = make(*size, dtype, ignored=0.1, seed=seed)
+        g = torch.Generator(device="cuda").manual_seed(seed)
+        return x, w, t, torch.exp2(-12.0 * torch.rand(t.shape, device="cuda", generator=g))
+
+    def step(x, w, t, up):
+        loss, st = apml.apml_linear_ce_forward(x, w, t, reduction="none", z_weight=1e-3)
+        return loss, *apml.apml_linear_ce_backward(st, x, w, t, up, reduction="none", z_weight=1e-3)
+
+    held = data(1)
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(stream):
+        step(*held)
+        stream.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=stream):
+            got = step(*held)
+    torch.cuda.synchronize()
+    for k in range(3):
+        new = data(20 + k)
+        for a, b in zip(held, new):
+            a.copy_(b)
+        want = step(*new)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(p, q) for p, q in zip(got, want))
