@@ -334,7 +334,9 @@ typedef enum { APML_REDUCE_NONE = 0, APML_REDUCE_SUM = 1, APML_REDUCE_MEAN = 2 }
  * ignored (the loss is 0 where all are). An ignored row adds nothing and gets a
  * zero gradient, whatever x holds there. A target outside [0, classes) other
  * than ignore_index gives a NaN loss for its row, NaN gradients of that row and
- * of w.
+ * of w. A row that counts and whose upstream gradient is 0 gets a zero gradient.
+ * Features of w, and of x in rows that count, have to be finite: an infinite one
+ * gives NaN in float32, whose products are made of pieces of the operands.
  */
 typedef struct apml_linear_ce_desc {
     uint32_t struct_size; /* sizeof(apml_linear_ce_desc) */
